@@ -234,7 +234,8 @@ def _plain_head(s):
     x = torch.zeros((n, kb * 128), device="cuda")
     x[:, :K] = s["hidden"].float()
     x = x.view(n, kb, 128)
-    scale = x.abs().amax(-1) / 448.0
+    scale = x.abs().amax(-1)
+    scale = scale / torch.full_like(scale, 448.0)  # a quotient in IEEE single precision (by a number, torch multiplies with its reciprocal)
     scale = torch.where(scale == 0, torch.ones_like(scale), scale)
     x = ((x / scale[..., None]).to(torch.float8_e4m3fn).float() * scale[..., None]).view(n, kb * 128)[:, :K]
     out = s["logits"]
@@ -339,7 +340,8 @@ def exact(case, seed):
         x = torch.zeros((n, K), **f64)
         for k in range(0, K, 128):
             b = piece[:, k:k + 128]
-            scale = b.abs().max(1, keepdim=True).values / 448.0
+            scale = b.abs().max(1, keepdim=True).values
+            scale = scale / torch.full_like(scale, 448.0)
             scale[scale == 0] = 1.0
             x[:, k:k + 128] = (b / scale).to(torch.float8_e4m3fn).double() * scale.double()
         for v in range(0, V, 4096):
