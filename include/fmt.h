@@ -401,6 +401,94 @@ fmt_status fmt_state_read_profile_series(fmt_state* s, int kind, float* ms_out, 
 fmt_status fmt_fill_mask_noalloc(const fmt_grammar* g, const uint32_t* charts_dev, const uint64_t* chart_offsets,
                                  uint32_t n, uint32_t* mask_dev, int32_t* status_dev, void* stream);
 
+/*
+ * The operators around the mask: the output head, which makes the logits, and what is read off the masked logits.  (The paper
+ * takes both as given: Figure 2 begins at the logits and ends at the token.)  They need no grammar and no fmt_state, allocate
+ * nothing, keep nothing from one call for the next, and may be captured into graphs and replayed, also several of them at a
+ * time on different streams.  A device pointer that the current device cannot reach (host memory that is not page-locked,
+ * another GPU's memory) is refused with FMT_ERR_INVALID_ARG, and so is one that is not aligned to its elements.  With rows = 0
+ * a call does nothing.  Outputs must not overlap inputs unless stated otherwise.  Columns beyond V or K, and rows beyond
+ * `rows`, are neither read nor written.
+ */
+
+/*
+ * Values in 8-bit floating point (e4m3: largest 448, no infinities) with an fp32 scale for each block of block_rows x 128:
+ *   scale = max |x| of the block / 448, or 1 where that quotient is 0;   q = x / scale, rounded to the nearest e4m3, ties to even
+ * (both quotients in IEEE single precision).  A block that holds a NaN or an infinity gets the scale NaN, and NaNs as values.
+ *   x_dev        [rows][cols], fmt_dtype, rows row_stride_elems apart
+ *   block_rows   1: hidden states, a scale for each row and 128 columns: scales_dev[block * scale_stride + row],
+ *                   scale_stride >= rows (the scales of one block of columns lie side by side)
+ *                128: weights, a scale for each 128 x 128: scales_dev[(row / 128) * scale_stride + block],
+ *                   scale_stride >= ceil(cols / 128)
+ *   q_dev        bytes, rows q_stride bytes apart; bytes beyond `cols` are left as they were
+ */
+fmt_status fmt_quantize_blocks(const void* x_dev, fmt_dtype dtype, uint32_t rows, uint32_t cols, size_t row_stride_elems,
+                               uint32_t block_rows, uint8_t* q_dev, size_t q_stride, float* scales_dev, size_t scale_stride,
+                               void* stream);
+
+/*
+ * The output head: logits of every row under its mask.
+ *   logits[i][v] = sum over blocks b of 128 columns: hidden_scales[b][i] * weight_scales[v / 128][b]
+ *                                                    * sum over k in block b: hidden[i][k] * weight[v][k]
+ * with e4m3 values and sums in fp32, rounded once to `dtype`; -inf (as fmt_apply_mask writes it) where bit v of row i's mask
+ * is 0.  Weights of 32 tokens in a row (a mask word) that no row may use are not read.
+ *   hidden_dev   [rows][K] e4m3 bytes and hidden_scales_dev, as fmt_quantize_blocks writes them with block_rows = 1
+ *   weight_dev   [V][K] e4m3 bytes and weight_scales_dev, as it writes them with block_rows = 128
+ *   hidden_stride, weight_stride  bytes from row to row, at least K, multiples of 16; both arrays 16-byte aligned
+ *   mask_dev     [rows][mask_stride_words] packed masks (fmt_fill_mask), or NULL: every token is allowed
+ * K at most 2^20, rows and V at most 2^24.  Every wait inside the kernel is a poll with an iteration limit; should one run out,
+ * the logits that are not computed become NaN.
+ */
+fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_stride, const float* hidden_scales_dev, size_t hidden_scale_stride,
+                           const uint8_t* weight_dev, size_t weight_stride, const float* weight_scales_dev, size_t weight_scale_stride,
+                           uint32_t rows, uint32_t V, uint32_t K, const uint32_t* mask_dev, size_t mask_stride_words,
+                           void* logits_dev, fmt_dtype dtype, size_t row_stride_elems, void* stream);
+
+/*
+ * Log probabilities under the mask: of given tokens, of the likeliest ones, and the entropy.  A row's distribution is
+ *   p(v) = exp((x[v] - M) / T) / S,   M = largest x,   S = sum of exp((x[v] - M) / T)
+ * over the tokens that its mask allows and whose logit is not -inf (so masked logits may be given instead of the mask).
+ *   mask_dev          packed masks or NULL; logits that a mask forbids are not looked at
+ *   temperature_dev   [rows] T or NULL (1)
+ *   tokens_dev        [rows][n_tokens] int32, n_tokens <= FMT_MAX_GIVEN_TOKENS; -1 is no token (log probability 0)
+ *   n_top             alternatives asked for, <= FMT_MAX_TOP
+ * Outputs, each of which may be NULL (dense arrays):
+ *   logprobs_dev      [rows][n_tokens] ln p of the given tokens, -inf for one that is not allowed
+ *   norm_dev          [rows][2] M and ln S: ln p(v) = (x[v] - M) / T - ln S
+ *   entropy_dev       [rows] -sum of p ln p, in nats
+ *   top_ids_dev       [rows][n_top] int32 the n_top tokens with the largest logits, largest first, of equal ones the lowest id;
+ *                     -1 where fewer are allowed.  With n_top = 1 these are the greedy tokens, as fmt_state_advance takes them
+ *   top_logprobs_dev  [rows][n_top] their ln p, -inf beside -1
+ *   status_dev        [rows] int32: FMT_OK, or FMT_ERR_INVALID_ARG: a given token is not in [-1, V) (its log probability is NaN,
+ *                     the others stand), or the temperature is not a positive finite number, or an allowed logit is NaN or
+ *                     +inf (all the row's outputs are NaN, its alternatives -1)
+ * A row without an allowed token: log probabilities -inf, M and ln S -inf, entropy 0, alternatives -1.
+ */
+#define FMT_MAX_GIVEN_TOKENS 32
+#define FMT_MAX_TOP 32
+fmt_status fmt_token_logprobs(const void* logits_dev, fmt_dtype dtype, uint32_t rows, uint32_t V, size_t row_stride_elems,
+                              const uint32_t* mask_dev, size_t mask_stride_words, const float* temperature_dev,
+                              const int32_t* tokens_dev, uint32_t n_tokens, uint32_t n_top, float* logprobs_dev, float* norm_dev,
+                              float* entropy_dev, int32_t* top_ids_dev, float* top_logprobs_dev, int32_t* status_dev, void* stream);
+
+/*
+ * The gradient of fmt_token_logprobs with respect to the logits, for a loss whose derivatives by a row's log probabilities
+ * and entropy are grad_logprobs_dev and grad_entropy_dev (either may be NULL: zeros):
+ *   grad[v] = (sum over given tokens t equal to v: g_t - p(v) * sum over t: g_t - g_H * p(v) * (ln p(v) + H)) / T
+ * and 0 where the token is not allowed or its logit is -inf.  The g_t of a given token does not count where it is -1, out of
+ * range, or its log probability is -inf.  A token given twice counts twice.
+ *   logits .. n_tokens  as in the forward call
+ *   norm_dev            the forward call's norm_dev; entropy_dev its entropy_dev (needed with grad_entropy_dev only)
+ *   grad_logits_dev     [rows][V] of the logits' dtype, rows grad_stride_elems apart; it may be the logits themselves, with their
+ *                       stride, which are overwritten then
+ * Rows that the forward call gave NaN get NaN where tokens are allowed.
+ */
+fmt_status fmt_token_logprobs_backward(const void* logits_dev, fmt_dtype dtype, uint32_t rows, uint32_t V, size_t row_stride_elems,
+                                       const uint32_t* mask_dev, size_t mask_stride_words, const float* temperature_dev,
+                                       const int32_t* tokens_dev, uint32_t n_tokens, const float* norm_dev, const float* entropy_dev,
+                                       const float* grad_logprobs_dev, const float* grad_entropy_dev, void* grad_logits_dev,
+                                       size_t grad_stride_elems, void* stream);
+
 const char* fmt_last_error(void);
 
 #ifdef __cplusplus

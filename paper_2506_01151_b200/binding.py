@@ -23,7 +23,8 @@ EXPORTS = [
     "fmt_compile", "fmt_json_schema_to_ebnf", "fmt_compile_json_schema", "fmt_grammar_destroy", "fmt_grammar_get_info", "fmt_grammar_copy_table", "fmt_grammar_automaton_match",
     "fmt_state_create", "fmt_state_destroy", "fmt_state_reset", "fmt_state_advance", "fmt_state_forced_bytes", "fmt_fill_mask",
     "fmt_apply_mask", "fmt_fill_and_apply", "fmt_state_cache_clear", "fmt_state_ci_cache_clear", "fmt_state_set_wait_limit", "fmt_state_copy_counters", "fmt_state_query", "fmt_state_copy_chart", "fmt_get_stats",
-    "fmt_state_set_profiling", "fmt_state_read_profile", "fmt_state_read_profile_series", "fmt_fill_mask_noalloc", "fmt_last_error",
+    "fmt_state_set_profiling", "fmt_state_read_profile", "fmt_state_read_profile_series", "fmt_fill_mask_noalloc",
+    "fmt_quantize_blocks", "fmt_head_logits", "fmt_token_logprobs", "fmt_token_logprobs_backward", "fmt_last_error",
 ]
 
 
@@ -108,6 +109,10 @@ def lib():
         L.fmt_state_read_profile.argtypes = [vp, C.POINTER(Profile)]
         L.fmt_state_read_profile_series.argtypes = [vp, C.c_int, vp, sz, C.POINTER(sz)]
         L.fmt_fill_mask_noalloc.argtypes = [vp, vp, vp, u32, vp, vp, vp]
+        L.fmt_quantize_blocks.argtypes = [vp, C.c_int, u32, u32, sz, u32, vp, sz, vp, sz, vp]
+        L.fmt_head_logits.argtypes = [vp, sz, vp, sz, vp, sz, vp, sz, u32, u32, u32, vp, sz, vp, C.c_int, sz, vp]
+        L.fmt_token_logprobs.argtypes = [vp, C.c_int, u32, u32, sz, vp, sz, vp, vp, u32, u32, vp, vp, vp, vp, vp, vp, vp]
+        L.fmt_token_logprobs_backward.argtypes = [vp, C.c_int, u32, u32, sz, vp, sz, vp, vp, u32, vp, vp, vp, vp, vp, sz, vp]
         L.fmt_last_error.restype = C.c_char_p
         for name in EXPORTS:
             if name not in ("fmt_grammar_destroy", "fmt_state_destroy", "fmt_last_error"):
@@ -364,3 +369,59 @@ def fill_mask_noalloc(grammar: Grammar, charts_dev, chart_offsets: Sequence[int]
     n = len(offs) - 1
     _check(lib().fmt_fill_mask_noalloc(grammar._h, _ptr(charts_dev), offs.ctypes.data, n, _ptr(mask_dev),
                                        _ptr(status_dev), _ptr(stream)))
+
+
+MAX_GIVEN_TOKENS = 32
+MAX_TOP = 32
+
+
+def quantize_blocks(x_dev, dtype: int, rows: int, cols: int, block_rows: int, q_dev, scales_dev, row_stride: Optional[int] = None,
+                    q_stride: Optional[int] = None, scale_stride: Optional[int] = None, stream=None):
+    """fmt_quantize_blocks: e4m3 bytes and a scale for each block of block_rows (1 or 128) x 128.
+    scales_dev: [ceil(cols/128), rows] for block_rows 1, [ceil(rows/128), ceil(cols/128)] for 128."""
+    rs = cols if row_stride is None else row_stride
+    qs = cols if q_stride is None else q_stride
+    ss = (rows if block_rows == 1 else (cols + 127) // 128) if scale_stride is None else scale_stride
+    _check(lib().fmt_quantize_blocks(_ptr(x_dev), dtype, rows, cols, rs, block_rows, _ptr(q_dev), qs, _ptr(scales_dev), ss, _ptr(stream)))
+
+
+def head_logits(hidden_dev, hidden_scales_dev, weight_dev, weight_scales_dev, logits_dev, dtype: int, rows: int, V: int, K: int,
+                mask_dev=None, hidden_stride: Optional[int] = None, hidden_scale_stride: Optional[int] = None,
+                weight_stride: Optional[int] = None, weight_scale_stride: Optional[int] = None, stride_words: Optional[int] = None,
+                row_stride: Optional[int] = None, stream=None):
+    """fmt_head_logits: the logits of e4m3 hidden states and weights (quantize_blocks) under packed masks."""
+    hs = K if hidden_stride is None else hidden_stride
+    hss = rows if hidden_scale_stride is None else hidden_scale_stride
+    ws = K if weight_stride is None else weight_stride
+    wss = (K + 127) // 128 if weight_scale_stride is None else weight_scale_stride
+    ms = (V + 31) // 32 if stride_words is None else stride_words
+    rs = V if row_stride is None else row_stride
+    _check(lib().fmt_head_logits(_ptr(hidden_dev), hs, _ptr(hidden_scales_dev), hss, _ptr(weight_dev), ws, _ptr(weight_scales_dev), wss,
+                                 rows, V, K, _ptr(mask_dev), ms, _ptr(logits_dev), dtype, rs, _ptr(stream)))
+
+
+def token_logprobs(logits_dev, dtype: int, rows: int, V: int, tokens_dev=None, n_tokens: int = 0, logprobs_dev=None, norm_dev=None,
+                   entropy_dev=None, n_top: int = 0, top_ids_dev=None, top_logprobs_dev=None, mask_dev=None,
+                   stride_words: Optional[int] = None, row_stride: Optional[int] = None, temperature_dev=None, status_dev=None,
+                   stream=None):
+    """fmt_token_logprobs: log probabilities of given tokens ([rows, n_tokens] int32), the normaliser ([rows, 2]), the entropy
+    and the n_top likeliest tokens of each row's distribution over what its mask allows."""
+    ms = (V + 31) // 32 if stride_words is None else stride_words
+    rs = V if row_stride is None else row_stride
+    _check(lib().fmt_token_logprobs(_ptr(logits_dev), dtype, rows, V, rs, _ptr(mask_dev), ms, _ptr(temperature_dev), _ptr(tokens_dev),
+                                    n_tokens, n_top, _ptr(logprobs_dev), _ptr(norm_dev), _ptr(entropy_dev), _ptr(top_ids_dev),
+                                    _ptr(top_logprobs_dev), _ptr(status_dev), _ptr(stream)))
+
+
+def token_logprobs_backward(logits_dev, dtype: int, rows: int, V: int, norm_dev, grad_logits_dev, tokens_dev=None, n_tokens: int = 0,
+                            grad_logprobs_dev=None, entropy_dev=None, grad_entropy_dev=None, mask_dev=None,
+                            stride_words: Optional[int] = None, row_stride: Optional[int] = None, grad_stride: Optional[int] = None,
+                            temperature_dev=None, stream=None):
+    """fmt_token_logprobs_backward: the logits' gradient from those of the log probabilities ([rows, n_tokens]) and the entropy
+    ([rows]), with the forward call's norm and entropy.  grad_logits_dev may be the logits."""
+    ms = (V + 31) // 32 if stride_words is None else stride_words
+    rs = V if row_stride is None else row_stride
+    gs = V if grad_stride is None else grad_stride
+    _check(lib().fmt_token_logprobs_backward(_ptr(logits_dev), dtype, rows, V, rs, _ptr(mask_dev), ms, _ptr(temperature_dev),
+                                             _ptr(tokens_dev), n_tokens, _ptr(norm_dev), _ptr(entropy_dev), _ptr(grad_logprobs_dev),
+                                             _ptr(grad_entropy_dev), _ptr(grad_logits_dev), gs, _ptr(stream)))

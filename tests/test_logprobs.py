@@ -1,0 +1,423 @@
+"""Log probabilities under the mask and their gradient (fmt_token_logprobs, fmt_token_logprobs_backward) against the formulas in
+64 bits, and what the two refuse.
+
+Tolerances, with u = 2^-24 (half a unit of fp32).  d = (x - M) / T takes three roundings: 3 u |d|, and exp turns that into the
+same relative error, plus 2 units of its own.  Sums of V terms are made of chains of at most V / 128 additions per thread and a
+tree: (V / 128 + 32) u relative for sums of terms of one sign.  So with A = V / 128 + 64 (the rest of the constants included):
+  ln p           u (4 |d| + A + 4 dm),       dm = the largest |d| whose exp is not 0 (at most 104)
+  entropy        u (A + 4 dm) (2 + H)        (ln S and -t / S are both not negative: nothing cancels)
+  gradient       p (u (4 |ln p| + A + 4 dm)) (|sum g| + |g_H| (|ln p| + H + 2)) / T + 4 u sum |g| / T (given tokens)
+and half a step of the output's type on top.
+"""
+import numpy as np
+import pytest
+
+import paper_2506_01151_b200 as fmt
+
+U = 2.0 ** -24
+gpu = pytest.mark.gpu
+
+
+def torch_():
+    import torch
+
+    return torch
+
+
+DEV = "cuda:0"
+
+
+class Inputs:
+    """Logits in rows of any stride from any address, packed masks, temperatures, tokens."""
+
+    def __init__(self, n, V, dtype="bf16", mask="mixed", stride=None, offset=0, heat=True, n_tokens=2, seed=0, mask_pad=0, scale=2.5):
+        torch = torch_()
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        self.n, self.V, self.n_tokens = n, V, n_tokens
+        self.dtype = fmt.BF16 if dtype == "bf16" else fmt.FP32
+        self.type = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.stride = V if stride is None else stride
+        self.store = torch.full((offset + max(n, 1) * self.stride + 8,), float("nan"), dtype=self.type, device=DEV)
+        self.logits = self.store[offset:].as_strided((n, V), (self.stride, 1))
+        self.logits.copy_((torch.randn((n, V), generator=g, device=DEV) * scale).to(self.type))
+        self.words = (V + 31) // 32
+        self.mask_stride = self.words + mask_pad
+        share = {"none": 1.0, "all": 1.0, "mixed": 0.5, "few": min(1.0, 3.0 / V)}[mask]
+        self.allow = torch.rand((n, V), generator=g, device=DEV) < share
+        self.masked = mask != "none"
+        self.temperature = 0.3 + torch.rand(n, generator=g, device=DEV) * 2 if heat else None
+        self.tokens = torch.randint(0, V, (n, n_tokens), generator=g, device=DEV, dtype=torch.int32)
+        self.g = torch.randn((n, n_tokens), generator=g, device=DEV)
+        self.gh = torch.randn(n, generator=g, device=DEV)
+
+    def mask(self):
+        """The packed masks; what lies behind a row's words is all ones, and so are the bits beyond V."""
+        torch = torch_()
+        if not self.masked:
+            return None
+        bits = torch.ones((self.n, self.mask_stride * 32), dtype=torch.int64, device=DEV)
+        bits[:, : self.V] = self.allow.long()
+        w = (bits.view(self.n, -1, 32) << torch.arange(32, device=DEV)).sum(-1)
+        return torch.where(w >= 1 << 31, w - (1 << 32), w).to(torch.int32)
+
+    def kw(self, **more):
+        return dict(dict(mask_dev=self.mask(), stride_words=self.mask_stride, row_stride=self.stride, temperature_dev=self.temperature), **more)
+
+    def forward(self, n_top=5, stream=None, into=None):
+        torch = torch_()
+        f = dict(dtype=torch.float32, device=DEV)
+        out = into or {
+            "logprobs": torch.full((self.n + 1, self.n_tokens), 77.0, **f), "norm": torch.full((self.n + 1, 2), 77.0, **f),
+            "entropy": torch.full((self.n + 1,), 77.0, **f), "ids": torch.full((self.n + 1, n_top), 77, dtype=torch.int32, device=DEV),
+            "tops": torch.full((self.n + 1, n_top), 77.0, **f), "status": torch.full((self.n + 1,), 77, dtype=torch.int32, device=DEV)}
+        fmt.token_logprobs(self.logits, self.dtype, self.n, self.V, tokens_dev=self.tokens, n_tokens=self.n_tokens, logprobs_dev=out["logprobs"],
+                           norm_dev=out["norm"], entropy_dev=out["entropy"], n_top=n_top, top_ids_dev=out["ids"], top_logprobs_dev=out["tops"],
+                           status_dev=out["status"], stream=stream, **self.kw())
+        return out
+
+    def backward(self, out, grad=None, in_place=False, grad_stride=None, with_g=True, with_h=True, stream=None):
+        torch = torch_()
+        gs = self.stride if in_place else (grad_stride or self.V)
+        if in_place:
+            grad = self.logits
+        elif grad is None:
+            self.grad_store = torch.full((self.n * gs + 8,), 77.0, dtype=self.type, device=DEV)
+            grad = self.grad_store.as_strided((self.n, self.V), (gs, 1))
+        fmt.token_logprobs_backward(self.logits, self.dtype, self.n, self.V, out["norm"], grad, tokens_dev=self.tokens, n_tokens=self.n_tokens,
+                                    grad_logprobs_dev=self.g if with_g else None, entropy_dev=out["entropy"],
+                                    grad_entropy_dev=self.gh if with_h else None, grad_stride=gs, stream=stream, **self.kw())
+        return grad
+
+    def reference(self, n_top=5, with_g=True, with_h=True):
+        """Everything in 64 bits from the definition, with the bounds above."""
+        torch = torch_()
+        n, V = self.n, self.V
+        x = self.logits.double()
+        allow = self.allow if self.masked else torch.ones_like(self.allow)
+        x = torch.where(allow, x, -torch.inf)
+        T = self.temperature.double()[:, None] if self.temperature is not None else torch.ones((n, 1), dtype=torch.float64, device=DEV)
+        allow = x != -torch.inf
+        bad = (~(x < torch.inf)).any(1) | ~((T[:, 0] > 0) & (T[:, 0] < torch.inf))
+        M = x.max(1, keepdim=True).values
+        none = M[:, 0] == -torch.inf
+        d = torch.where(allow, (x - M) / T, -torch.inf)
+        S = torch.exp(d).sum(1, keepdim=True)
+        lp = torch.where(allow, d - torch.log(S), -torch.inf)
+        p = torch.where(allow, torch.exp(lp), 0.0)
+        H = -torch.where(p > 0, p * lp, 0.0).sum(1)
+        tok = self.tokens.long()
+        inside = (tok >= 0) & (tok < V)
+        at = tok.clamp(0, V - 1)
+        got = torch.where(inside, torch.gather(lp, 1, at), torch.where(tok == -1, 0.0, torch.nan))
+        got = torch.where(bad[:, None] & (tok != -1), torch.nan, got)
+        order = torch.sort(x + 0.0, dim=1, descending=True, stable=True)
+        k = min(n_top, V)
+        ids = torch.full((n, n_top), -1, dtype=torch.int64, device=DEV)
+        tops = torch.full((n, n_top), -torch.inf, dtype=torch.float64, device=DEV)
+        ids[:, :k] = torch.where(order.values[:, :k] == -torch.inf, -1, order.indices[:, :k])
+        tops[:, :k] = torch.where(ids[:, :k] >= 0, torch.gather(lp, 1, order.indices[:, :k]), -torch.inf)
+        ids[bad], tops[bad] = -1, torch.nan
+        norm = torch.cat([M, torch.log(S)], 1)
+        norm[bad] = torch.nan
+        H = torch.where(bad, torch.nan, torch.where(none, 0.0, H))
+        status = torch.where(bad | ((tok < -1) | (tok >= V)).any(1), fmt.ERR_INVALID_ARG, fmt.FMT_OK)
+        g = torch.where(inside & (torch.gather(lp, 1, at).float() > -torch.inf), self.g.double() * with_g, 0.0)
+        gh = self.gh.double()[:, None] * with_h
+        total = g.sum(1, keepdim=True)
+        grad = -p * total - gh * p * torch.where(p > 0, lp + H[:, None], 0.0)
+        grad.scatter_add_(1, at, g)
+        grad = torch.where(allow, torch.where(bad[:, None], torch.nan, grad / T), 0.0)
+        A = V / 128 + 64
+        dm = torch.where(torch.exp(d) > 1e-45, d.abs(), 0.0).nan_to_num(0, 0, 0).amax(1, keepdim=True).clamp(max=104)
+        ad = d.abs().nan_to_num(0, 0, 0)
+        tol_lp = U * (4 * ad + A + 4 * dm)
+        e = U * (4 * lp.abs().nan_to_num(0, 0, 0) + A + 4 * dm)
+        ag = torch.zeros_like(p).scatter_add_(1, at, g.abs())
+        tol_grad = (p * e * (g.abs().sum(1, keepdim=True) + gh.abs() * (lp.abs().nan_to_num(0, 0, 0) + H.abs()[:, None] + 2)) + 4 * U * ag) / T
+        return {"logprobs": got, "norm": norm, "entropy": H, "ids": ids, "tops": tops, "status": status, "grad": grad,
+                "tol": {"logprobs": torch.gather(tol_lp, 1, at), "norm": torch.cat([U * M.abs(), U * (A + 4 * dm)], 1),
+                        "entropy": U * (A + 4 * dm[:, 0]) * (2 + H), "tops": torch.gather(tol_lp, 1, ids.clamp(min=0)), "grad": tol_grad}}
+
+
+def near(got, want, tol, what, half=U):
+    torch = torch_()
+    if got.dtype == torch.float32:  # what is beyond the type's range (the lowest logit over a temperature below 1) is rounded to an infinity
+        want = torch.where(torch.isinf(want.float()), want.float().double(), want)
+    got = got.double()
+    odd = ~torch.isfinite(want)
+    same = torch.where(torch.isnan(want), torch.isnan(got), got == want)
+    assert bool(same[odd].all()), (what, "infinities or NaN", torch.nonzero(~same & odd)[:4].tolist())
+    err = (got - want).abs()[~odd]
+    limit = (tol + half * want.abs() + 1e-40)[~odd]
+    assert bool((err <= limit).all()), (what, float((err / limit).max()), float(err.max()))
+
+
+def check_forward(i, out, n_top=5):
+    torch = torch_()
+    want = i.reference(n_top)
+    n = i.n
+    for k in ("logprobs", "norm", "entropy", "tops"):
+        near(out[k][:n], want[k], want["tol"][k].nan_to_num(0, 0, 0), k)
+        assert bool((out[k][n:] == 77).all()), "behind the last row"
+    assert torch.equal(out["ids"][:n].long(), want["ids"]) and torch.equal(out["status"][:n].long(), want["status"])
+    assert bool((out["ids"][n:] == 77).all()) and bool((out["status"][n:] == 77).all())
+    return want
+
+
+def check_backward(i, grad, want):
+    half = torch_().finfo(i.type).eps / 2
+    tiny = 2.0 ** -133 if i.dtype == fmt.BF16 else 2.0 ** -149  # what is left of denormals
+    near(grad, want["grad"], want["tol"]["grad"].nan_to_num(0, 0, 0) + tiny, "grad", half)
+
+
+SHAPES = [(1, 1), (3, 2), (2, 31), (5, 33), (1, 512), (7, 1000), (4, 4099), (37, 50001), (200, 777), (2, 128256), (300, 9001)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("mask", ["none", "mixed", "few"])
+@pytest.mark.parametrize("n,V", SHAPES)
+def test_forward_and_gradient(n, V, mask, dtype):
+    i = Inputs(n, V, dtype, mask, seed=n * 7 + V, heat=V % 2 == 1)
+    out = i.forward()
+    want = check_forward(i, out)
+    check_backward(i, i.backward(out), want)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("offset,pad", [(0, 0), (1, 0), (3, 5), (5, 1), (7, 9), (8, 16)])
+@pytest.mark.parametrize("V", [7, 250, 4099, 20000])
+def test_rows_begin_at_any_address(V, offset, pad, dtype):
+    i = Inputs(6, V, dtype, "mixed", stride=V + pad, offset=offset, mask_pad=pad % 3, seed=offset + V)
+    before = i.store.clone()
+    out = i.forward(9)
+    want = check_forward(i, out, 9)
+    grad = i.backward(out, grad_stride=V + pad)
+    check_backward(i, grad, want)
+    torch = torch_()
+    edge = torch.ones_like(i.grad_store, dtype=torch.bool)
+    edge.as_strided((6, V), (V + pad, 1))[:] = False
+    assert bool((i.grad_store[edge] == 77).all()), "between the rows"
+    assert torch.equal(before.view(torch.uint8), i.store.view(torch.uint8)), "the logits are only read"
+    check_backward(i, i.backward(out, in_place=True), want)
+    edge = torch.ones_like(i.store, dtype=torch.bool)
+    edge[offset:].as_strided((6, V), (V + pad, 1))[:] = False
+    assert bool(torch.isnan(i.store[edge]).all()), "between the rows"
+
+
+@gpu
+@pytest.mark.parametrize("V", [40, 6000, 60000])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_that_are_out_of_the_ordinary(V, dtype):
+    torch = torch_()
+    i = Inputs(17, V, dtype, "mixed", n_tokens=6, seed=V)
+    low = torch.finfo(i.type).min
+    nan, inf = float("nan"), float("inf")
+    x, a = i.logits, i.allow
+    a[0] = False                                      # nothing allowed
+    a[1] = False; a[1, V - 1] = True                  # one token, the last
+    a[2] = True; x[2] = 1.5                           # all alike
+    a[3] = True; x[3] = low                           # all the type's lowest value
+    x[4] = torch.where(torch.rand(V, device=DEV) < 0.9, torch.full_like(x[4], low), x[4])
+    a[5] = True; x[5] = -inf                          # nothing left, and no mask says so
+    x[6][~a[6]] = nan                                 # what is not allowed is not looked at
+    x[7][~a[7]] = inf
+    a[8, 3] = True; x[8, 3] = nan                     # an allowed NaN
+    a[9, 4] = True; x[9, 4] = inf
+    i.temperature[10], i.temperature[11], i.temperature[12], i.temperature[13] = 0.0, -1.0, nan, inf
+    i.tokens[14] = torch.tensor([-1, V, -2, 5, 5, 2 ** 31 - 1], device=DEV, dtype=torch.int32)
+    a[14, 5] = True
+    i.tokens[15] = 7; a[15, 7] = True                 # one token six times
+    a[16] = True; x[16] = torch.where(torch.arange(V, device=DEV) % 2 == 0, 0.0, -0.0).to(i.type)  # 0 and -0 are equal
+    out = i.forward(7)
+    want = check_forward(i, out, 7)
+    assert out["ids"][16].tolist() == list(range(7)) and out["ids"][2].tolist() == list(range(7))
+    check_backward(i, i.backward(out), want)
+
+
+@gpu
+@pytest.mark.parametrize("n_top", [1, 2, 31, 32])
+@pytest.mark.parametrize("order", ["up", "down", "ties", "one place", "stripes"])
+def test_alternatives_wherever_they_lie(order, n_top):
+    """The largest logits side by side, far apart, in one thread's part, among many equals."""
+    torch = torch_()
+    V = 30011
+    i = Inputs(3, V, "fp32", "none", heat=False, n_tokens=1, seed=n_top)
+    at = torch.arange(V, device=DEV, dtype=torch.float32)
+    x = {"up": at / V, "down": -at / V, "ties": (at % 13).floor() - (at % 7 == 3) * 5, "one place": torch.where((at >= 9000) & (at < 9050), 9050 - at, at * 1e-6),
+         "stripes": torch.where(at % 1024 == 5, 3 + at / V, at * 1e-6)}[order]
+    i.logits[:] = x
+    i.logits[1] = x.flip(0)
+    i.logits[2] = torch.roll(x, 12345)
+    check_forward(i, i.forward(n_top), n_top)
+    j = Inputs(3, V, "bf16", "few", heat=False, n_tokens=1, seed=n_top)  # fewer than asked for
+    check_forward(j, j.forward(n_top), n_top)
+
+
+@gpu
+@pytest.mark.parametrize("n_tokens", [0, 1, 32])
+@pytest.mark.parametrize("with_g,with_h", [(True, False), (False, True), (False, False)])
+def test_gradients_that_are_not_given(n_tokens, with_g, with_h):
+    i = Inputs(5, 3001, "fp32", "mixed", n_tokens=n_tokens, seed=n_tokens)
+    out = i.forward(0)
+    want = i.reference(0, with_g, with_h)
+    check_backward(i, i.backward(out, with_g=with_g, with_h=with_h), want)
+
+
+@gpu
+def test_outputs_that_are_not_asked_for():
+    torch = torch_()
+    i = Inputs(9, 5003, "bf16", "mixed", n_tokens=1)
+    full = i.forward(1)
+    ids = torch.full((9,), 77, dtype=torch.int32, device=DEV)
+    fmt.token_logprobs(i.logits, i.dtype, 9, i.V, n_top=1, top_ids_dev=ids, **i.kw())
+    assert torch.equal(ids, full["ids"][:9, 0])
+    lp = torch.full((9, 1), 77.0, device=DEV)
+    fmt.token_logprobs(i.logits, i.dtype, 9, i.V, tokens_dev=i.tokens, n_tokens=1, logprobs_dev=lp, n_top=7, **i.kw())
+    assert torch.equal(lp, full["logprobs"][:9])
+    fmt.token_logprobs(i.logits, i.dtype, 9, i.V, **i.kw())  # nothing asked for
+    fmt.token_logprobs(i.logits, i.dtype, 0, i.V, tokens_dev=i.tokens, n_tokens=1, logprobs_dev=lp, **i.kw())
+    assert torch.equal(lp, full["logprobs"][:9])
+
+
+@gpu
+def test_gradient_by_differences():
+    """Central differences of the 64-bit loss, apart from the formula of the gradient."""
+    torch = torch_()
+    i = Inputs(2, 60, "fp32", "mixed", n_tokens=3, seed=5)
+    i.allow[:, :8] = True
+    i.tokens[:] = torch.tensor([[1, 1, 5], [0, -1, 7]], dtype=torch.int32, device=DEV)
+    out = i.forward(0)
+    grad = i.backward(out).double()
+    T, ok = i.temperature.double()[:, None], i.tokens.long() >= 0
+
+    def loss(x):
+        lp = torch.log_softmax(torch.where(i.allow, x, -torch.inf) / T, 1)
+        p = lp.exp()
+        h = -(p * lp.masked_fill(~i.allow, 0)).sum(1)
+        return (torch.where(ok, torch.gather(lp, 1, i.tokens.long().clamp(min=0)), 0.0) * i.g.double()).sum(1) + i.gh.double() * h
+
+    x, step = i.logits.double(), 1e-5
+    for v in range(60):
+        e = torch.zeros_like(x)
+        e[:, v] = step
+        diff = (loss(x + e) - loss(x - e)) / (2 * step)
+        # the third derivative is below 10 here, so the difference is off by less than 10 step^2; the rest are 64-bit roundings
+        assert float((grad[:, v] - diff).abs().max()) < 2e-8 + 64 * U * 10, v
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_farther_apart_than_32_bits(dtype):
+    torch = torch_()
+    stride = (1 << 30) + 7
+    i = Inputs(4, 1500, dtype, "mixed", stride=stride, seed=3)
+    out = i.forward()
+    want = check_forward(i, out)
+    check_backward(i, i.backward(out, in_place=True), want)
+    del i
+    torch.cuda.empty_cache()
+
+
+@gpu
+def test_captured_replayed_and_on_other_streams():
+    """Two graphs of the same call with other inputs, replayed at the same time on two streams, several times."""
+    torch = torch_()
+    ins = [Inputs(n, 40001, "bf16", "mixed", n_tokens=2, seed=n) for n in (3, 150)]
+    outs = [i.forward() for i in ins]
+    grads = [i.backward(o) for i, o in zip(ins, outs)]
+    wants = [check_forward(i, o) for i, o in zip(ins, outs)]
+    masks = [i.mask() for i in ins]
+    for i, m in zip(ins, masks):
+        i.mask = lambda m=m: m
+    torch.cuda.synchronize()
+    graphs, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i, o, gr, s in zip(ins, outs, grads, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            h = torch.cuda.current_stream().cuda_stream
+            i.forward(into=o, stream=h)
+            i.backward(o, grad=gr, stream=h)
+        graphs.append(g)
+    for _ in range(5):
+        for o, gr in zip(outs, grads):
+            for k in ("logprobs", "norm", "entropy", "tops"):
+                o[k].fill_(77.0)
+            o["ids"].fill_(77), o["status"].fill_(77), gr.fill_(77.0)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for i, o, gr, w in zip(ins, outs, grads, wants):
+            check_forward(i, o)
+            check_backward(i, gr, w)
+
+
+@gpu
+def test_the_same_call_gives_the_same_bits():
+    torch = torch_()
+    i = Inputs(64, 50001, "bf16", "mixed", n_tokens=3, seed=1)
+    first = i.forward(20)
+    grad = i.backward(first).clone()
+    for _ in range(3):
+        again = i.forward(20)
+        assert all(torch.equal(first[k], again[k]) for k in first)
+        assert torch.equal(grad, i.backward(again))
+
+
+def refused(f, *a, **kw):
+    with pytest.raises(fmt.FmtError) as e:
+        f(*a, **kw)
+    assert e.value.code == fmt.ERR_INVALID_ARG
+    return str(e.value)
+
+
+def test_refusals():
+    """Every one of these is turned down on the host, before anything reaches a GPU."""
+    P = 1 << 20  # never read
+    f = lambda **kw: fmt.token_logprobs(**dict(dict(logits_dev=P, dtype=fmt.BF16, rows=2, V=100, norm_dev=P), **kw))
+    b = lambda **kw: fmt.token_logprobs_backward(**dict(dict(logits_dev=P, dtype=fmt.BF16, rows=2, V=100, norm_dev=P, grad_logits_dev=P + 4096), **kw))
+    for call in (f, b):
+        refused(call, logits_dev=None)
+        refused(call, dtype=2)
+        refused(call, V=0)
+        refused(call, V=(1 << 30) + 1)
+        refused(call, rows=(1 << 24) + 1)
+        refused(call, row_stride=99)
+        refused(call, mask_dev=P, stride_words=3)
+        refused(call, n_tokens=33, tokens_dev=P)
+        refused(call, n_tokens=1)
+        refused(call, logits_dev=P + 1)
+        refused(call, dtype=fmt.FP32, logits_dev=P + 2)
+        refused(call, mask_dev=P + 2)
+        refused(call, temperature_dev=P + 1)
+        refused(call, n_tokens=1, tokens_dev=P + 3)
+        refused(call, norm_dev=P + 2)
+    refused(f, n_top=33, top_ids_dev=P)
+    refused(f, status_dev=P + 2)
+    refused(f, n_top=3, top_ids_dev=P + 1)
+    refused(b, norm_dev=None)
+    refused(b, grad_logits_dev=None)
+    refused(b, grad_stride=99)
+    refused(b, grad_entropy_dev=P)
+    refused(b, grad_logits_dev=P, row_stride=100, grad_stride=101)
+    refused(b, grad_logits_dev=P + 4097)
+
+
+@gpu
+def test_memory_that_the_device_cannot_reach_is_refused():
+    torch = torch_()
+    i = Inputs(2, 64, "fp32", "mixed", n_tokens=1)
+    host = torch.zeros((2, 64))
+    norm = torch.zeros((2, 2), device=DEV)
+    refused(fmt.token_logprobs, host, fmt.FP32, 2, 64, norm_dev=norm)
+    refused(fmt.token_logprobs, i.logits, fmt.FP32, 2, 64, norm_dev=host)
+    refused(fmt.token_logprobs, i.logits, fmt.FP32, 2, 64, norm_dev=norm, mask_dev=torch.zeros((2, 2), dtype=torch.int32))
+    refused(fmt.token_logprobs_backward, i.logits, fmt.FP32, 2, 64, norm, host)
+    status = torch.full((2,), 77, dtype=torch.int32).pin_memory()  # page-locked memory is reached
+    fmt.token_logprobs(i.logits, fmt.FP32, 2, 64, norm_dev=norm, status_dev=status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0, 0]
