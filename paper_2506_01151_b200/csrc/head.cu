@@ -59,32 +59,45 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T* x, uint32_t rows
 
 // ------------------------------------------------------------------------------------------------ the product
 //
-// D[token of the vocabulary][row] on the tensor cores, one block of 128 columns at a time: four tcgen05.mma of 32 columns each make
-// the block's 128 x N sums in tensor memory, from where eight warps take them, multiply them with the block's two scales and add
-// them up in registers.  (Scales of any value cannot ride along in the instruction, whose own are powers of two.)  The vocabulary
-// is the M side: a decoding step has few rows and very many tokens, and M is 128 whatever N is.
+// On the tensor cores, one block of 128 columns at a time: four tcgen05.mma of 32 columns each make the block's sums in tensor
+// memory, from where eight warps take them, multiply them with the block's two scales and add them up in registers.  (Scales of
+// any value cannot ride along in the instruction, whose own are powers of two.)
 //
-// A thread block to an SM.  The vocabulary goes to the blocks in slabs of 32 tokens, a word of the mask and a quarter of a tile:
-// slab s to block s mod C.  A block makes a list of its slabs that some row may use, and takes four at a time, wherever they lie;
-// the others are written as -inf and their weights not read.  Work is even to a slab (128,256 tokens: 27 or 28 of 4,008 to each of 148).
+// A thread block to an SM.  The vocabulary goes to the blocks in slabs of 32 tokens, a word of the mask: four at a time, one block
+// after the other, and what is left then one by one, so that work is even to a slab (128,256 tokens: 27 or 28 of 4,008 to each of
+// 148).  A block makes a list of its slabs that some row may use, and takes several at a time, wherever they lie; the others are
+// written as -inf and their weights not read.  Four slabs that follow one another are copied in one go: the copying thread needs
+// 150 cycles for each copy it asks for (2,048 rows x 128,256 x 4,096: 1,616 us with a copy for each slab).
 //
-// Warps: 0 copies tiles to shared memory (TMA, a ring of stages), 1 issues the products, 2 copies the scales (a ring of their own,
-// as they are needed later than the tiles), 4 to 11 add up and write.
+// Few rows (up to 64): the vocabulary is the M side, four slabs to the 128 lanes of tensor memory, and 16, 32 or 64 rows the N
+// side: M is 128 whatever is there, and a decoding step has many tokens and few rows.  More rows: 128 rows are the M side and eight
+// slabs the N side.  A lane is a row then, and one product of scales serves the 32 sums of a slab.
+//
+// Warps: 0 copies weights and 3 hidden states to shared memory (TMA, a ring of stages), 1 issues the products, 2 copies the scales
+// (a ring of their own, as they are needed later), 4 to 11 add up and write.
 
-constexpr uint32_t SLAB = 32, TILE_SLABS = 4;
+constexpr uint32_t SLAB = 32;
 constexpr uint32_t HEAD_THREADS = 384, ADD_WARPS = 8;
 constexpr uint32_t LIST = 512;        // slabs of a block that are looked at in one go
 constexpr uint32_t SCALE_SLOTS = 8;
 constexpr uint32_t SLAB_BYTES = SLAB * BLOCK;
-constexpr uint32_t WAIT_POLLS = 1u << 20;  // of at most 2 us each
+constexpr uint32_t WAIT_POLLS = 1u << 20;
+constexpr uint32_t WIDE_ROWS = 128;        // the M side's
+constexpr uint32_t TURN = 16;              // words of a row that a warp turns round in shared memory on their way out
 
-template <uint32_t N>
+template <uint32_t ROWS, bool WIDE>
 struct HeadShape {
-  static constexpr uint32_t stages = N == 256 ? 4 : N == 128 ? 6 : N == 64 ? 8 : 10;
-  static constexpr uint32_t bufs = N == 256 ? 2 : N == 128 ? 4 : 8;  // of tensor memory, N columns each
-  static constexpr uint32_t stage_bytes = TILE_SLABS * SLAB_BYTES + N * BLOCK;
-  static constexpr uint32_t slot_floats = N + TILE_SLABS;
-  static constexpr uint32_t smem = 1024 + stages * stage_bytes + SCALE_SLOTS * slot_floats * 4;
+  static constexpr uint32_t slabs = WIDE ? 8 : 4;                     // of a tile
+  static constexpr uint32_t columns = WIDE ? slabs * SLAB : ROWS;     // of tensor memory
+  static constexpr uint32_t depth = WIDE ? 1 : 2;                     // blocks of columns that make a stage: each round of waits costs some 400 cycles
+  static constexpr uint32_t stages = WIDE ? 4 : ROWS == 64 ? 4 : 5;
+  static constexpr uint32_t bufs = WIDE ? 2 : 4;                      // of tensor memory, depth x columns each
+  static constexpr uint32_t block_bytes = slabs * SLAB_BYTES + ROWS * BLOCK;
+  static constexpr uint32_t stage_bytes = depth * block_bytes;
+  static constexpr uint32_t block_floats = ROWS + slabs;              // scales
+  static constexpr uint32_t slot_floats = depth * block_floats;
+  static constexpr uint32_t own_floats = WIDE ? 32 * (TURN + 1) : 0;  // of an adding warp
+  static constexpr uint32_t smem = 1024 + stages * stage_bytes + (SCALE_SLOTS * slot_floats + ADD_WARPS * own_floats) * 4;
 };
 
 struct HeadArgs {
@@ -100,11 +113,11 @@ struct HeadArgs {
 };
 
 struct HeadShared {
-  uint64_t full[10], empty[10], sums_full[8], sums_empty[8], scales_full[SCALE_SLOTS], scales_empty[SCALE_SLOTS];
-  uint32_t tmem, n_live, n_dead;
+  uint64_t full[5], empty[5], sums_full[4], sums_empty[4];
+  uint32_t tmem, n_live, n_dead, issued[4];
   volatile uint32_t gave_up;
   uint32_t bits[LIST / 32];
-  uint16_t live[LIST], dead[LIST];
+  uint32_t live[LIST], dead[LIST];
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -119,8 +132,8 @@ __device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
 }
 __device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
   uint32_t done;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
-               : "=r"(done) : "r"(smem_addr(b)), "r"(parity), "r"(2000u) : "memory");
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(done) : "r"(smem_addr(b)), "r"(parity) : "memory");
   return done != 0u;
 }
 // Waits until the barrier's phase of this parity is over.  False: given up, here or by another warp of the block.
@@ -131,8 +144,25 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, HeadShare
   S.gave_up = 1u;
   return false;
 }
+// The same for a whole warp, which goes on either way and looks at gave_up when it is through with a tile.
+__device__ __forceinline__ void bar_wait_on(uint64_t* b, uint32_t parity, HeadShared& S) {
+  if (!bar_test(b, parity)) {
+    uint32_t i = 0;
+    while (!bar_test(b, parity) && !S.gave_up)
+      if (++i == WAIT_POLLS) S.gave_up = 1u;
+  }
+  __syncwarp();
+}
 __device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity) {  // the same after giving up, for what is in flight
   for (uint32_t i = 0; i < WAIT_POLLS && !bar_test(b, parity); ++i) {}
+}
+
+// One thread of a warp that is all here.  (The compiler knows what this is: operands of copies and products that it sees in one
+// thread alone go into uniform registers as they are; under `lane == 0` it makes loops around each of them.)
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+  return yes != 0u;
 }
 
 // A place in a ring and how often it has been round.
@@ -161,6 +191,7 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
+__device__ __forceinline__ void block_sync() { asm volatile("bar.sync 1, %0;" ::"n"(HEAD_THREADS) : "memory"); }  // from wherever a warp is
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
@@ -169,49 +200,58 @@ __device__ __forceinline__ void tmem_read(uint32_t addr, float (&v)[COLS]);
 #define R4(i) "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3])
 template <>
 __device__ __forceinline__ void tmem_read<8>(uint32_t addr, float (&v)[8]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : R4(0), R4(4) : "r"(addr));
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : R4(0), R4(4) : "r"(addr) : "memory");
 }
 template <>
 __device__ __forceinline__ void tmem_read<16>(uint32_t addr, float (&v)[16]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-               : R4(0), R4(4), R4(8), R4(12) : "r"(addr));
+               : R4(0), R4(4), R4(8), R4(12) : "r"(addr) : "memory");
 }
 template <>
 __device__ __forceinline__ void tmem_read<32>(uint32_t addr, float (&v)[32]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
                "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-               : R4(0), R4(4), R4(8), R4(12), R4(16), R4(20), R4(24), R4(28) : "r"(addr));
+               : R4(0), R4(4), R4(8), R4(12), R4(16), R4(20), R4(24), R4(28) : "r"(addr) : "memory");
 }
 #undef R4
-// The values that a read of tensor memory gave may be used from here on.
-template <uint32_t COLS>
-__device__ __forceinline__ void tmem_read_done(float (&v)[COLS]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (uint32_t i = 0; i < COLS; ++i) asm volatile("" : "+f"(v[i]));
+// What has been read from tensor memory may be used from here on, by what stays behind it (add_products).
+__device__ __forceinline__ void tmem_read_done() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Two products at a time.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+  return p;
 }
+__device__ __forceinline__ void add_products(uint64_t& sum, float lo, float hi, uint64_t scales) {
+  asm volatile("{\n.reg .b64 x;\nmov.b64 x, {%1, %2};\nfma.rn.f32x2 %0, x, %3, %0;\n}" : "+l"(sum) : "f"(lo), "f"(hi), "l"(scales));
+}
+__device__ __forceinline__ float part(uint64_t p, uint32_t i) { return __uint_as_float((uint32_t)(p >> (32u * i))); }
 
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(uint16_t* p, float x) { *p = __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 
-template <typename T, uint32_t N>
-__global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const HeadArgs A) {
-  using Shape = HeadShape<N>;
-  constexpr uint32_t COLS = N / 2;                   // of a tile, to each of the adding warps
-  constexpr uint32_t CHUNK = COLS < 32 ? COLS : 32;  // read from tensor memory in one go
-  constexpr uint32_t TMEM = Shape::bufs * N;
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+
+template <typename T, uint32_t ROWS, bool WIDE>
+__global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap wmap4,
+                                                               const __grid_constant__ CUtensorMap xmap, const HeadArgs A) {
+  using Shape = HeadShape<ROWS, WIDE>;
+  constexpr uint32_t SLABS = Shape::slabs, DEPTH = Shape::depth, BUF = DEPTH * Shape::columns, TMEM = Shape::bufs * BUF;
   extern __shared__ uint8_t raw[];
   __shared__ HeadShared S;
   const uint32_t tiles_at = (smem_addr(raw) + 1023u) & ~1023u;
   float* const scales = reinterpret_cast<float*>(raw + (tiles_at - smem_addr(raw)) + Shape::stages * Shape::stage_bytes);
   const uint32_t tid = threadIdx.x, warp = tid / 32u, lane = tid % 32u;
-  const uint32_t n_slabs = (A.V + SLAB - 1) / SLAB, n_blocks = (A.K + BLOCK - 1) / BLOCK, row_tiles = (A.rows + N - 1) / N;
+  const uint32_t n_slabs = (A.V + SLAB - 1) / SLAB, n_blocks = (A.K + BLOCK - 1) / BLOCK, row_tiles = (A.rows + ROWS - 1) / ROWS;
 
   if (tid == 0) {
-    for (uint32_t i = 0; i < Shape::stages; ++i) bar_init(&S.full[i], 1), bar_init(&S.empty[i], 1);
-    for (uint32_t i = 0; i < Shape::bufs; ++i) bar_init(&S.sums_full[i], 1), bar_init(&S.sums_empty[i], ADD_WARPS);
-    for (uint32_t i = 0; i < SCALE_SLOTS; ++i) bar_init(&S.scales_full[i], 32), bar_init(&S.scales_empty[i], ADD_WARPS);
-    S.gave_up = 0u;
+    for (uint32_t i = 0; i < Shape::stages; ++i) bar_init(&S.full[i], 2), bar_init(&S.empty[i], 1);
+    for (uint32_t i = 0; i < Shape::bufs; ++i) bar_init(&S.sums_full[i], 2), bar_init(&S.sums_empty[i], ADD_WARPS);
+    S.gave_up = 0u, S.issued[0] = S.issued[1] = S.issued[2] = S.issued[3] = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -226,17 +266,22 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
   Ring<Shape::stages> stage;
   Ring<Shape::bufs> buf;
   Ring<SCALE_SLOTS> slot;
-  uint32_t issued = 0;  // tiles under way, or done (warps 0 and 1)
+  uint32_t issued = 0;  // stages filled (warps 0 and 3) or used (warp 1)
   bool failed = false;
 
-  for (uint32_t first = blockIdx.x; first < n_slabs; first += LIST * gridDim.x) {
-    // which of the block's slabs some row may use
-    const uint32_t here = min(LIST, (n_slabs - first + gridDim.x - 1) / gridDim.x);
+  const uint32_t fours = n_slabs / (4u * gridDim.x);  // groups of four that every block has
+  const uint32_t n_mine = 4u * fours + (n_slabs - 4u * fours * gridDim.x + gridDim.x - 1u - blockIdx.x) / gridDim.x;
+  auto slab_no = [&](uint32_t i) {  // the block's i-th
+    return i < 4u * fours ? 4u * (i / 4u * gridDim.x + blockIdx.x) + i % 4u : i * gridDim.x + blockIdx.x;
+  };
+  // The block's slabs from the first-th on that some row may use, and the others.  All threads.
+  auto list_slabs = [&](uint32_t first) {
+    const uint32_t here = min(LIST, n_mine - first);
     if (tid < LIST / 32) S.bits[tid] = A.mask ? 0u : 0xFFFFFFFFu;
-    __syncthreads();
+    block_sync();
     if (A.mask)
       for (uint32_t i = warp; i < here; i += HEAD_THREADS / 32) {
-        const uint32_t* m = A.mask + first + (size_t)i * gridDim.x;
+        const uint32_t* m = A.mask + slab_no(first + i);
         uint32_t any = 0u;
         for (uint32_t r0 = 0; r0 < A.rows && !any; r0 += 256) {
 #pragma unroll
@@ -246,164 +291,293 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
         }
         if (lane == 0 && any) atomicOr(&S.bits[i / 32], 1u << (i % 32));
       }
-    __syncthreads();
+    block_sync();
     if (warp == 0) {
       uint32_t n_live = 0, n_dead = 0;
       for (uint32_t i = 0; i < here; i += 32) {
         const uint32_t word = S.bits[i / 32], in = here - i < 32u ? (1u << (here - i)) - 1u : 0xFFFFFFFFu;
-        const uint32_t alive = word & in, gone = ~word & in, before = (1u << lane) - 1u;
-        if ((alive >> lane) & 1u) S.live[n_live + __popc(alive & before)] = (uint16_t)(i + lane);
-        if ((gone >> lane) & 1u) S.dead[n_dead + __popc(gone & before)] = (uint16_t)(i + lane);
+        const uint32_t alive = word & in, gone = ~word & in, before = (1u << lane) - 1u, no = slab_no(first + i + lane);
+        if ((alive >> lane) & 1u) S.live[n_live + __popc(alive & before)] = no;
+        if ((gone >> lane) & 1u) S.dead[n_dead + __popc(gone & before)] = no;
         n_live += __popc(alive), n_dead += __popc(gone);
       }
       if (lane == 0) S.n_live = n_live, S.n_dead = n_dead;
     }
-    __syncthreads();
-    const uint32_t n_live = S.n_live;
-    auto slab = [&](uint32_t i) { return first + (uint32_t)S.live[i] * gridDim.x; };
+    block_sync();
+  };
 
-    if (warp == 0) {
-      if (lane == 0)
-        for (uint32_t g = 0; g < n_live && !failed; g += TILE_SLABS)
+  if (warp < 4) {
+    if (WIDE) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // 384 threads of 168 registers: 256 x 216 + 128 x 72 are no more
+    for (uint32_t first = 0; first < n_mine; first += LIST) {
+      list_slabs(first);
+      const uint32_t n_live = S.n_live;
+      if (warp == 0 && elected()) {
+        for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
           for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
-            const uint32_t count = min(TILE_SLABS, n_live - g);
-            uint32_t y[TILE_SLABS];
+            const uint32_t count = min(SLABS, n_live - g);
+            uint32_t y[SLABS / 4], whole = 0u;  // of four slabs: the first one's rows, whether the others follow
 #pragma unroll
-            for (uint32_t i = 0; i < TILE_SLABS; ++i) y[i] = slab(g + (i < count ? i : 0u)) * SLAB;
-            for (uint32_t b = 0; b < n_blocks; ++b) {
+            for (uint32_t i = 0; i < SLABS / 4; ++i) {
+              y[i] = 0u;
+              if (4u * i + 3u < count) {
+                y[i] = S.live[g + 4u * i] * SLAB;
+                if (S.live[g + 4u * i + 3u] * SLAB == y[i] + 3u * SLAB) whole |= 1u << i;
+              }
+            }
+            for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
               if (!bar_wait(&S.empty[stage.at], stage.round ^ 1u, S)) {
                 failed = true;
                 break;
               }
-              const uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
+              const uint32_t blocks = min(DEPTH, n_blocks - b);
+              uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
               uint64_t* bar = &S.full[stage.at];
-              bar_expect(bar, count * SLAB_BYTES + N * BLOCK);
+              bar_expect(bar, blocks * count * SLAB_BYTES);
+              for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) {
 #pragma unroll
-              for (uint32_t i = 0; i < TILE_SLABS; ++i)
-                if (i < count) tma_load(&wmap, bar, at + i * SLAB_BYTES, b * BLOCK, y[i]);
-              tma_load(&xmap, bar, at + TILE_SLABS * SLAB_BYTES, b * BLOCK, j * N);
+                for (uint32_t i = 0; i < SLABS / 4; ++i) {
+                  if ((whole >> i) & 1u) tma_load(&wmap4, bar, at + 4u * i * SLAB_BYTES, k * BLOCK, y[i]);
+                  else
+                    for (uint32_t q = 4u * i; q < min(4u * i + 4u, count); ++q) tma_load(&wmap, bar, at + q * SLAB_BYTES, k * BLOCK, S.live[g + q] * SLAB);
+                }
+              }
               ++issued;
               stage.next();
             }
           }
-    } else if (warp == 1) {
-      if (lane == 0) {
-        // e4m3 x e4m3 into fp32, both K-major, N columns, 128 lanes
-        constexpr uint32_t idesc = 1u << 4 | (N >> 3) << 17 | (128u >> 4) << 24;
-        const uint32_t tiles = ((n_live + TILE_SLABS - 1) / TILE_SLABS) * ((row_tiles + gridDim.y - 1 - blockIdx.y) / gridDim.y);
-        for (uint32_t t = 0; t < tiles && !failed; ++t)
-          for (uint32_t b = 0; b < n_blocks; ++b) {
-            if (!bar_wait(&S.sums_empty[buf.at], buf.round ^ 1u, S) || !bar_wait(&S.full[stage.at], stage.round, S)) {
-              failed = true;
-              break;
+      } else if (warp == 3 && elected()) {
+        for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
+          for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y)
+            for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
+              if (!bar_wait(&S.empty[stage.at], stage.round ^ 1u, S)) {
+                failed = true;
+                break;
+              }
+              const uint32_t blocks = min(DEPTH, n_blocks - b);
+              uint32_t at = tiles_at + stage.at * Shape::stage_bytes + SLABS * SLAB_BYTES;
+              bar_expect(&S.full[stage.at], blocks * ROWS * BLOCK);
+              for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) tma_load(&xmap, &S.full[stage.at], at, k * BLOCK, j * ROWS);
+              ++issued;
+              stage.next();
             }
-            after_sync();
-            const uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
-            const uint64_t a = tile_desc(at), x = tile_desc(at + TILE_SLABS * SLAB_BYTES);
+      } else if (warp == 1 && elected()) {
+        for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
+          for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
+            // e4m3 x e4m3 into fp32, both K-major, 128 lanes
+            const uint32_t columns = WIDE ? min(SLABS, n_live - g) * SLAB : ROWS;
+            const uint32_t idesc = 1u << 4 | (columns >> 3) << 17 | (128u >> 4) << 24;
+            for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
+              if (!bar_wait(&S.sums_empty[buf.at], buf.round ^ 1u, S) || !bar_wait(&S.full[stage.at], stage.round, S)) {
+                failed = true;
+                break;
+              }
+              after_sync();
+              const uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
+              const uint64_t w = tile_desc(at), x = tile_desc(at + SLABS * SLAB_BYTES);
 #pragma unroll
-            for (uint32_t k = 0; k < 4; ++k) mma(S.tmem + buf.at * N, a + 2 * k, x + 2 * k, idesc, k != 0);
-            mma_commit(&S.empty[stage.at]);
-            mma_commit(&S.sums_full[buf.at]);
-            ++issued;
-            stage.next(), buf.next();
+              for (uint32_t k = 0; k < DEPTH; ++k)
+                if (k == 0 || b + k < n_blocks) {
+#pragma unroll
+                  for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t more = (k * Shape::block_bytes + 32u * i) >> 4;
+                    mma(S.tmem + buf.at * BUF + k * Shape::columns, (WIDE ? x : w) + more, (WIDE ? w : x) + more, idesc, i != 0);
+                  }
+                }
+              mma_commit(&S.empty[stage.at]);
+              mma_commit(&S.sums_full[buf.at]);
+              ++issued;
+              stage.next(), buf.next();
+            }
           }
-      }
-    } else if (warp == 2) {
-      for (uint32_t g = 0; g < n_live && !failed; g += TILE_SLABS)
-        for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
-          const uint32_t count = min(TILE_SLABS, n_live - g), r0 = j * N;
-          const float* wp = A.ws + (size_t)(slab(g + (lane < count ? lane : 0u)) / TILE_SLABS) * A.ws_stride;
-          for (uint32_t b = 0; b < n_blocks; ++b) {
-            if (__any_sync(0xFFFFFFFFu, !bar_wait(&S.scales_empty[slot.at], slot.round ^ 1u, S))) {
-              failed = true;
-              break;
-            }
-            const uint32_t dst = smem_addr(scales + slot.at * Shape::slot_floats);
-            const float* xp = A.xs + (size_t)b * A.xs_stride + r0;
+      } else if (warp == 2) {
+        // A stage's scales are asked for AHEAD stages early, and their being there is one of the two things that sums_full waits for.
+        constexpr uint32_t AHEAD = SCALE_SLOTS - Shape::bufs;
+        const uint32_t total = (n_live + SLABS - 1) / SLABS * ((row_tiles + gridDim.y - 1 - blockIdx.y) / gridDim.y) * ((n_blocks + DEPTH - 1) / DEPTH);
+        uint32_t g = 0, j = blockIdx.y, b = 0;
+        for (uint32_t t = 0; t < total + AHEAD; ++t) {
+          if (t >= AHEAD) bar_wait_on(&S.sums_empty[buf.at], buf.round ^ 1u, S);
+          if (t < total) {
+            const uint32_t count = min(SLABS, n_live - g), r0 = j * ROWS;
+            for (uint32_t k = b; k < min(b + DEPTH, n_blocks); ++k) {
+              const uint32_t dst = smem_addr(scales + slot.at * Shape::slot_floats + (k - b) * Shape::block_floats);
+              const float* xp = A.xs + (size_t)k * A.xs_stride + r0;
 #pragma unroll
-            for (uint32_t i = 0; i < (N + 31u) / 32u; ++i) {
-              const uint32_t c = i * 32u + lane;
-              if (c < N && r0 + c < A.rows)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + c * 4u), "l"(xp + c) : "memory");
+              for (uint32_t i = 0; i < (ROWS + 31u) / 32u; ++i) {
+                const uint32_t c = i * 32u + lane;
+                if (c < ROWS && r0 + c < A.rows) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + c * 4u), "l"(xp + c) : "memory");
+              }
+              if (lane < count)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + (ROWS + lane) * 4u),
+                             "l"(A.ws + (size_t)(S.live[g + lane] * SLAB / BLOCK) * A.ws_stride + k) : "memory");
             }
-            if (lane < count) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + (N + lane) * 4u), "l"(wp + b) : "memory");
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&S.scales_full[slot.at])) : "memory");
             slot.next();
+            b += DEPTH;
+            if (b >= n_blocks) {
+              b = 0, j += gridDim.y;
+              if (j >= row_tiles) j = blockIdx.y, g += SLABS;
+            }
+          }
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          if (t >= AHEAD) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(&S.sums_full[buf.at]);
+            buf.next();
           }
         }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (warp >= 4) {
-      const uint32_t quarter = warp % 4u, half = (warp - 4u) / 4u;  // 32 lanes of tensor memory, half of the columns
-      T* const logits = static_cast<T*>(A.logits);
+      }
+      __syncwarp();
+      block_sync();  // the lists are made anew
+    }
+    // nothing of this block's is in flight when it ends: every copy has landed and every product is through
+    if (issued) S.issued[warp] = issued;  // (the threads that were elected)
+    __syncwarp();
+    asm volatile("bar.sync 2, 128;" ::: "memory");
+    if (warp == 0 && lane == 0) {
+      const uint32_t some = min(S.issued[0], S.issued[3]), most = max(S.issued[0], S.issued[3]);
+      for (uint32_t i = some; i < most; ++i) bar_arrive(&S.full[i % Shape::stages]);  // stages that only one of the two copying threads came to fill
+      for (uint32_t i = most - min(most, Shape::stages); i < most; ++i) bar_drain(&S.full[i % Shape::stages], i / Shape::stages & 1u);
+    }
+    if (warp == 1 && lane == 0)
+      for (uint32_t i = S.issued[1] - min(S.issued[1], Shape::stages); i < S.issued[1]; ++i) bar_drain(&S.empty[i % Shape::stages], i / Shape::stages & 1u);
+  } else {
+    if (WIDE) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const uint32_t quarter = warp % 4u, half = (warp - 4u) / 4u;  // 32 lanes of tensor memory, half of the columns
+    T* const logits = static_cast<T*>(A.logits);
+    float* const own = scales + SCALE_SLOTS * Shape::slot_floats + (warp - 4u) * Shape::own_floats;
+    const float minus_inf = -__int_as_float(0x7F800000), nan = __int_as_float(0x7FC00000);
+    for (uint32_t first = 0; first < n_mine; first += LIST) {
+      list_slabs(first);
+      const uint32_t n_live = S.n_live;
       // the slabs that no row may use
       for (uint32_t i = warp - 4u; i < S.n_dead; i += ADD_WARPS) {
-        const uint32_t v = (first + (uint32_t)S.dead[i] * gridDim.x) * SLAB + lane;
+        const uint32_t v = S.dead[i] * SLAB + lane;
         if (v < A.V)
-          for (uint32_t r = blockIdx.y; r < A.rows; r += gridDim.y) put(logits + (size_t)r * A.row_stride + v, -__int_as_float(0x7F800000));
+          for (uint32_t r = blockIdx.y; r < A.rows; r += gridDim.y) put(logits + (size_t)r * A.row_stride + v, minus_inf);
       }
-      for (uint32_t g = 0; g < n_live; g += TILE_SLABS)
+      for (uint32_t g = 0; g < n_live; g += SLABS)
         for (uint32_t j = blockIdx.y; j < row_tiles; j += gridDim.y) {
-          const bool mine = quarter < n_live - g;
-          const uint32_t s = slab(mine ? g + quarter : g), v = s * SLAB + lane;
-          float sum[COLS];
+          constexpr uint32_t COLS = Shape::columns / 2;      // of the tile, this warp's
+          constexpr uint32_t CHUNK = COLS < 32 ? COLS : 32;  // read from tensor memory in one go
+          constexpr uint32_t READS = DEPTH * COLS / CHUNK;   // of a stage; an even number
+          constexpr uint32_t FACTORS = WIDE ? 4 : DEPTH * COLS / 2;
+          const uint32_t count = n_live - g;                 // slabs that are there
+          const uint32_t mine = WIDE ? (count > half * 4u ? min(4u, count - half * 4u) : 0u) : quarter < count ? 1u : 0u;
+          uint64_t sum[COLS / 2];
 #pragma unroll
-          for (uint32_t c = 0; c < COLS; ++c) sum[c] = 0.0f;
-          for (uint32_t b = 0; b < n_blocks; ++b) {
-            if (failed || __any_sync(0xFFFFFFFFu, !bar_wait(&S.sums_full[buf.at], buf.round, S) || !bar_wait(&S.scales_full[slot.at], slot.round, S))) {
-              failed = true;
-              break;
-            }
+          for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = 0;
+          // One piece is read while the one before is added, the first of the next stage (if it is there) with the last of this one.
+          float d[2][CHUNK];
+          const uint32_t lanes = S.tmem + (quarter * 32u << 16) + half * COLS;
+          auto read = [&](uint32_t r) { tmem_read<CHUNK>(lanes + buf.at * BUF + r * CHUNK / COLS * Shape::columns + r * CHUNK % COLS, d[r % 2]); };
+          auto first_read = [&] {
+            bar_wait_on(&S.sums_full[buf.at], buf.round, S);
             after_sync();
-            if (mine) {
-              const float* sc = scales + slot.at * Shape::slot_floats;
-              const float w = sc[N + quarter];
-              const float* x = sc + half * COLS;
-              const uint32_t from = S.tmem + (quarter * 32u << 16) + buf.at * N + half * COLS;
+            read(0);
+          };
+          first_read();
+          for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
+            uint64_t by[FACTORS];  // the products of two scales
+            const float* sc = scales + slot.at * Shape::slot_floats;
+            if (WIDE) {  // a row's scale times its slabs'
+              const float x = sc[quarter * 32u + lane];
+              const float4 w = *reinterpret_cast<const float4*>(sc + ROWS + half * 4u);
+              by[0] = pair(x * w.x, x * w.x), by[1 % FACTORS] = pair(x * w.y, x * w.y);
+              by[2 % FACTORS] = pair(x * w.z, x * w.z), by[3 % FACTORS] = pair(x * w.w, x * w.w);
+            } else {  // the slab's scale times its rows'
 #pragma unroll
-              for (uint32_t c0 = 0; c0 < COLS; c0 += CHUNK) {
-                float d[CHUNK];
-                tmem_read<CHUNK>(from + c0, d);
-                tmem_read_done<CHUNK>(d);
+              for (uint32_t k = 0; k < DEPTH; ++k) {
+                const float w = sc[k * Shape::block_floats + ROWS + quarter];
 #pragma unroll
-                for (uint32_t c = 0; c < CHUNK; c += 4) {
-                  const float4 f = *reinterpret_cast<const float4*>(x + c0 + c);
-                  sum[c0 + c] = fmaf(d[c], f.x * w, sum[c0 + c]);
-                  sum[c0 + c + 1] = fmaf(d[c + 1], f.y * w, sum[c0 + c + 1]);
-                  sum[c0 + c + 2] = fmaf(d[c + 2], f.z * w, sum[c0 + c + 2]);
-                  sum[c0 + c + 3] = fmaf(d[c + 3], f.w * w, sum[c0 + c + 3]);
+                for (uint32_t c = 0; c < COLS; c += 4) {
+                  const float4 x = *reinterpret_cast<const float4*>(sc + k * Shape::block_floats + half * COLS + c);
+                  by[(k * COLS + c) / 2 % FACTORS] = pair(x.x * w, x.y * w), by[((k * COLS + c) / 2 + 1) % FACTORS] = pair(x.z * w, x.w * w);
                 }
               }
             }
-            before_sync();
-            __syncwarp();
-            if (lane == 0) bar_arrive(&S.sums_empty[buf.at]), bar_arrive(&S.scales_empty[slot.at]);
-            buf.next(), slot.next();
+#pragma unroll
+            for (uint32_t r = 0; r < READS; ++r) {
+              tmem_read_done();
+              if (r + 1 < READS) {
+                read(r + 1);
+              } else {
+                before_sync();
+                __syncwarp();
+                if (lane == 0) bar_arrive(&S.sums_empty[buf.at]);
+                buf.next(), slot.next();
+                if (b + DEPTH < n_blocks) first_read();
+              }
+              constexpr uint32_t PER = COLS / CHUNK;  // reads of a block of columns
+              if (r < PER || b + r / PER < n_blocks) {
+#pragma unroll
+                for (uint32_t c = 0; c < CHUNK; c += 2)
+                  add_products(sum[(r % PER * CHUNK + c) / 2], d[r % 2][c], d[r % 2][c + 1], by[WIDE ? r : (r * CHUNK + c) / 2]);
+              }
+            }
           }
-          if (!mine) continue;
-          const uint32_t r0 = j * N + half * COLS;
+          const bool failed = S.gave_up != 0u;
+          if (WIDE) {
+            // a lane holds 32 tokens of a row for each slab: turned round, 16 tokens at a time, so that a warp writes them side by side
+            constexpr uint32_t TOKENS = TURN * 4 / sizeof(T);  // 16 words of a row
+            const uint32_t r0 = j * ROWS + quarter * 32u, rows_here = r0 < A.rows ? min(32u, A.rows - r0) : 0u;
+            const bool by_words = ((reinterpret_cast<uintptr_t>(logits) | A.row_stride * sizeof(T)) & 3u) == 0;
+            uint32_t* const words = reinterpret_cast<uint32_t*>(own);
 #pragma unroll
-          for (uint32_t c0 = 0; c0 < COLS; c0 += CHUNK) {
-            if (r0 + c0 >= A.rows) break;
-            uint32_t word = 0xFFFFFFFFu;  // lane c holds the mask's word of row c
-            if (A.mask && lane < CHUNK && r0 + c0 + lane < A.rows) word = __ldg(A.mask + (size_t)(r0 + c0 + lane) * A.mask_stride + s);
+            for (uint32_t i = 0; i < 4; ++i) {
+              if (i >= mine || !rows_here) break;
+              const uint32_t s = S.live[g + half * 4u + i];
+              const uint32_t word = !A.mask ? 0xFFFFFFFFu : lane < rows_here ? __ldg(A.mask + (size_t)(r0 + lane) * A.mask_stride + s) : 0u;
 #pragma unroll
-            for (uint32_t c = 0; c < CHUNK; ++c) {
-              const uint32_t m = __shfl_sync(0xFFFFFFFFu, word, c);
-              const float y = !((m >> lane) & 1u) ? -__int_as_float(0x7F800000) : failed ? __int_as_float(0x7FC00000) : sum[c0 + c];
-              if (r0 + c0 + c < A.rows && v < A.V) put(logits + (size_t)(r0 + c0 + c) * A.row_stride + v, y);
+              for (uint32_t t = 0; t < SLAB; t += TOKENS) {
+                auto masked = [&](uint32_t c) {
+                  const float y = failed ? nan : part(sum[(i * SLAB + t + c) / 2], c % 2);
+                  return (word >> (t + c)) & 1u ? y : minus_inf;
+                };
+#pragma unroll
+                for (uint32_t c = 0; c < TURN; ++c)
+                  words[lane * (TURN + 1) + c] = sizeof(T) == 4 ? __float_as_uint(masked(c)) : two_bf16(masked(2 * c % TOKENS), masked((2 * c + 1) % TOKENS));
+                __syncwarp();
+                if (by_words) {
+                  const uint32_t c = lane % TURN, v = s * SLAB + t + c * (4 / sizeof(T));
+                  T* to = logits + (size_t)(r0 + lane / TURN) * A.row_stride + v;
+                  const bool all = v + 4 / sizeof(T) <= A.V, some = v < A.V;
+#pragma unroll
+                  for (uint32_t r = lane / TURN; r < 32u; r += 32u / TURN, to += 2 * A.row_stride) {
+                    const uint32_t y = words[r * (TURN + 1) + c];
+                    if (r < rows_here) {
+                      if (all) *reinterpret_cast<uint32_t*>(to) = y;
+                      else if (some) *reinterpret_cast<uint16_t*>(to) = (uint16_t)y;
+                    }
+                  }
+                } else {  // bf16 in rows that begin at any address
+                  const uint32_t v = s * SLAB + t + lane;
+                  T* to = logits + (size_t)r0 * A.row_stride + v;
+#pragma unroll 8
+                  for (uint32_t r = 0; r < 32u; ++r, to += A.row_stride) {
+                    const uint16_t y = reinterpret_cast<const uint16_t*>(words + r * (TURN + 1))[lane];
+                    if (r < rows_here && v < A.V) *reinterpret_cast<uint16_t*>(to) = y;
+                  }
+                }
+                __syncwarp();
+              }
+            }
+          } else if (mine) {
+            const uint32_t s = S.live[g + quarter], v = s * SLAB + lane, r0 = j * ROWS + half * COLS;
+#pragma unroll
+            for (uint32_t c0 = 0; c0 < COLS; c0 += CHUNK) {
+              if (r0 + c0 >= A.rows) break;
+              uint32_t word = 0xFFFFFFFFu;  // lane c holds the mask's word of row c
+              if (A.mask && lane < CHUNK && r0 + c0 + lane < A.rows) word = __ldg(A.mask + (size_t)(r0 + c0 + lane) * A.mask_stride + s);
+#pragma unroll
+              for (uint32_t c = 0; c < CHUNK; ++c) {
+                const uint32_t m = __shfl_sync(0xFFFFFFFFu, word, c);
+                const float y = !((m >> lane) & 1u) ? minus_inf : failed ? nan : part(sum[(c0 + c) / 2], c % 2);
+                if (r0 + c0 + c < A.rows && v < A.V) put(logits + (size_t)(r0 + c0 + c) * A.row_stride + v, y);
+              }
             }
           }
         }
-    }
-    __syncthreads();  // the lists are made anew
-  }
-
-  // nothing of this block's is in flight when it ends: every copy has landed and every product is through
-  if (warp <= 1 && lane == 0) {
-    uint64_t* const bars = warp == 0 ? S.full : S.empty;
-    for (uint32_t i = 0; i < Shape::stages; ++i) {
-      const uint32_t uses = issued / Shape::stages + (i < issued % Shape::stages ? 1u : 0u);
-      if (uses) bar_drain(&bars[i], (uses - 1u) & 1u);
+      block_sync();
     }
   }
   before_sync();
@@ -436,35 +610,34 @@ struct HeadOperands {
   size_t hidden_stride, weight_stride;
 };
 
-template <typename T, uint32_t N>
+template <typename T, uint32_t ROWS, bool WIDE>
 fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, cudaStream_t st) {
-  CUtensorMap wmap, xmap;
-  if (!encode_tiled() || !byte_map(&wmap, O.weight, A.K, A.V, O.weight_stride, SLAB) || !byte_map(&xmap, O.hidden, A.K, A.rows, O.hidden_stride, N)) {
+  using Shape = HeadShape<ROWS, WIDE>;
+  CUtensorMap wmap, wmap4, xmap;
+  if (!encode_tiled() || !byte_map(&wmap, O.weight, A.K, A.V, O.weight_stride, SLAB) || !byte_map(&wmap4, O.weight, A.K, A.V, O.weight_stride, 4 * SLAB) ||
+      !byte_map(&xmap, O.hidden, A.K, A.rows, O.hidden_stride, ROWS)) {
     set_last_error("the operands cannot be described to the copy engine");
     return FMT_ERR_CUDA;
   }
-  auto* k = head_kernel<T, N>;
-  if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, HeadShape<N>::smem)) return launch_result(e);
+  auto* k = head_kernel<T, ROWS, WIDE>;
+  if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::smem)) return launch_result(e);
   // Rows that need several tiles: a block takes all of them for its slabs (the weights come from L2 after the first), unless
-  // the slabs divide badly among the blocks; then the tiles of rows are dealt out, too.  A tile costs the same however few
-  // of its four slabs are there.
-  const uint32_t slabs = (A.V + SLAB - 1) / SLAB, row_tiles = (A.rows + N - 1) / N;
+  // the slabs divide badly among the blocks; then the tiles of rows are dealt out, too.
+  const uint32_t slabs = (A.V + SLAB - 1) / SLAB, row_tiles = (A.rows + ROWS - 1) / ROWS;
   uint32_t split = 1, least = 0xFFFFFFFFu;
   for (uint32_t y = 1; y <= row_tiles && y <= sms; ++y) {
-    const uint32_t x = std::min(sms / y, slabs);
-    const uint32_t cost = ((slabs + x - 1) / x + TILE_SLABS - 1) / TILE_SLABS * ((row_tiles + y - 1) / y);
-    if (cost < least) least = cost, split = y;
+    const uint32_t x = std::min(sms / y, slabs), each = (slabs + x - 1) / x, turns = (row_tiles + y - 1) / y;
+    if (each * turns < least) least = each * turns, split = y;
   }
-  return launch_result(launch_overlapped(k, dim3(std::min(sms / split, slabs), split), dim3(HEAD_THREADS), HeadShape<N>::smem, st, wmap, xmap, A));
+  return launch_result(launch_overlapped(k, dim3(std::min(sms / split, slabs), split), dim3(HEAD_THREADS), Shape::smem, st, wmap, wmap4, xmap, A));
 }
 
 template <typename T>
 fmt_status head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, cudaStream_t st) {
-  if (A.rows <= 16) return launch_head<T, 16>(O, A, sms, st);
-  if (A.rows <= 32) return launch_head<T, 32>(O, A, sms, st);
-  if (A.rows <= 64) return launch_head<T, 64>(O, A, sms, st);
-  if (A.rows <= 128) return launch_head<T, 128>(O, A, sms, st);
-  return launch_head<T, 256>(O, A, sms, st);
+  if (A.rows <= 16) return launch_head<T, 16, false>(O, A, sms, st);
+  if (A.rows <= 32) return launch_head<T, 32, false>(O, A, sms, st);
+  if (A.rows <= 64) return launch_head<T, 64, false>(O, A, sms, st);
+  return launch_head<T, WIDE_ROWS, true>(O, A, sms, st);
 }
 
 }  // namespace
