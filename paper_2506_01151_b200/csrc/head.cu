@@ -18,7 +18,6 @@ namespace {
 constexpr uint32_t BLOCK = 128;  // columns (and, of weights, rows) that share a scale
 
 __device__ __forceinline__ float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-__device__ __forceinline__ float to_f32(float x) { return x; }
 
 // The scale of a block from the bits of its largest |x|: bits of magnitudes are ordered as the magnitudes are, infinities and
 // NaNs above them all.
@@ -32,29 +31,60 @@ __device__ __forceinline__ uint8_t to_e4m3(float x, float scale) {  // a NaN bec
   return (uint8_t)__nv_cvt_float_to_fp8(__fdiv_rn(x, scale), __NV_SATFINITE, __NV_E4M3);
 }
 
-// A thread block to a block of ROWS x 128 values.
+// Four values of a row in one go where they are whole and aligned, else one by one; what is behind the row's end is 0.
+__device__ __forceinline__ float4 load4(const uint16_t* x, uint32_t n, bool aligned) {
+  if (aligned && n >= 4) {
+    const uint2 u = *reinterpret_cast<const uint2*>(x);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
+  }
+  return make_float4(n > 0 ? to_f32(x[0]) : 0.0f, n > 1 ? to_f32(x[1]) : 0.0f, n > 2 ? to_f32(x[2]) : 0.0f, n > 3 ? to_f32(x[3]) : 0.0f);
+}
+__device__ __forceinline__ float4 load4(const float* x, uint32_t n, bool aligned) {
+  if (aligned && n >= 4) return *reinterpret_cast<const float4*>(x);
+  return make_float4(n > 0 ? x[0] : 0.0f, n > 1 ? x[1] : 0.0f, n > 2 ? x[2] : 0.0f, n > 3 ? x[3] : 0.0f);
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+__device__ __forceinline__ void store4(uint8_t* q, uint32_t n, bool aligned, float4 x, float scale) {
+  const uint32_t v = to_e4m3(x.x, scale) | (uint32_t)to_e4m3(x.y, scale) << 8 | (uint32_t)to_e4m3(x.z, scale) << 16 | (uint32_t)to_e4m3(x.w, scale) << 24;
+  if (aligned && n >= 4) *reinterpret_cast<uint32_t*>(q) = v;
+  else
+    for (uint32_t i = 0; i < n && i < 4; ++i) q[i] = (uint8_t)(v >> (8u * i));
+}
+
+// Hidden states: a warp to 128 values of a row, four to a lane.  Weights: a thread block to 128 x 128, 16 rows to a warp, which keeps
+// them in registers until the block's largest is known.  Either way a value is read once.
+constexpr uint32_t QUANTIZE_WARPS = 8;
 template <typename T, uint32_t ROWS>
-__global__ void __launch_bounds__(256) quantize_kernel(const T* x, uint32_t rows, uint32_t cols, size_t row_stride, uint8_t* q,
-                                                       size_t q_stride, float* scales, size_t scale_stride) {
+__global__ void __launch_bounds__(QUANTIZE_WARPS * 32) quantize_kernel(const T* x, uint32_t rows, uint32_t cols, size_t row_stride, uint8_t* q,
+                                                                       size_t q_stride, float* scales, size_t scale_stride) {
   before_me();
-  __shared__ uint32_t most;
-  const uint32_t r0 = blockIdx.x * ROWS, b = blockIdx.y, c0 = b * BLOCK;
-  if (threadIdx.x == 0) most = 0u;
-  __syncthreads();
-  const uint32_t n = min(ROWS, rows - r0) * BLOCK;
+  constexpr uint32_t EACH = ROWS == 1 ? 1 : ROWS / QUANTIZE_WARPS;  // rows of a warp
+  __shared__ uint32_t most[QUANTIZE_WARPS];
+  const uint32_t warp = threadIdx.x / 32u, lane = threadIdx.x % 32u, blocks = (cols + BLOCK - 1) / BLOCK;
+  const uint64_t unit = ROWS == 1 ? (uint64_t)blockIdx.x * QUANTIZE_WARPS + warp : blockIdx.x;
+  const uint32_t b = (uint32_t)(unit % blocks), c = b * BLOCK + lane * 4u, left = c < cols ? cols - c : 0u;
+  const uint64_t group = unit / blocks;  // of ROWS rows
+  const uint64_t r0 = ROWS == 1 ? group : group * ROWS + warp * EACH;
+  const bool x_aligned = ((reinterpret_cast<uintptr_t>(x) | row_stride * sizeof(T)) & (4u * sizeof(T) - 1u)) == 0;
+  const bool q_aligned = ((reinterpret_cast<uintptr_t>(q) | q_stride) & 3u) == 0;
+  float4 v[EACH];
   uint32_t amax = 0u;
-  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-    const uint32_t c = c0 + i % BLOCK;
-    if (c < cols) amax = max(amax, __float_as_uint(to_f32(x[(size_t)(r0 + i / BLOCK) * row_stride + c])) & 0x7FFFFFFFu);
+#pragma unroll
+  for (uint32_t i = 0; i < EACH; ++i) v[i] = load4(x + (r0 + i) * row_stride + c, r0 + i < rows ? left : 0u, x_aligned);
+#pragma unroll
+  for (uint32_t i = 0; i < EACH; ++i) amax = max(max(max(amax, magnitude(v[i].x)), max(magnitude(v[i].y), magnitude(v[i].z))), magnitude(v[i].w));
+  amax = __reduce_max_sync(0xFFFFFFFFu, amax);
+  if (ROWS > 1) {
+    if (lane == 0) most[warp] = amax;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < QUANTIZE_WARPS; ++i) amax = max(amax, most[i]);
   }
-  atomicMax(&most, amax);
-  __syncthreads();
-  const float scale = block_scale(most);
-  if (threadIdx.x == 0) scales[ROWS == 1 ? (size_t)b * scale_stride + r0 : (size_t)blockIdx.x * scale_stride + b] = scale;
-  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-    const uint32_t c = c0 + i % BLOCK;
-    if (c < cols) q[(size_t)(r0 + i / BLOCK) * q_stride + c] = to_e4m3(to_f32(x[(size_t)(r0 + i / BLOCK) * row_stride + c]), scale);
-  }
+  const float scale = block_scale(amax);
+  if (r0 < rows && lane == 0 && (ROWS == 1 || warp == 0)) scales[ROWS == 1 ? (size_t)b * scale_stride + r0 : (size_t)group * scale_stride + b] = scale;
+#pragma unroll
+  for (uint32_t i = 0; i < EACH; ++i)
+    if (r0 + i < rows) store4(q + (r0 + i) * q_stride + c, left, q_aligned, v[i], scale);
 }
 
 // ------------------------------------------------------------------------------------------------ the product
@@ -654,15 +684,17 @@ extern "C" fmt_status fmt_quantize_blocks(const void* x_dev, fmt_dtype dtype, ui
   if (misaligned(x_dev, dtype == FMT_BF16 ? 2 : 4) || misaligned(scales_dev, 4)) return refuse("a pointer is not aligned to its elements");
   if (rows == 0) return FMT_OK;
   if (fmt_status s = reachable({x_dev, q_dev, scales_dev})) return s;
-  const dim3 grid((rows + block_rows - 1) / block_rows, (cols + BLOCK - 1) / BLOCK);
+  const uint64_t units = (uint64_t)((rows + block_rows - 1) / block_rows) * ((cols + BLOCK - 1) / BLOCK), per = block_rows == 1 ? QUANTIZE_WARPS : 1;
+  if ((units + per - 1) / per > 0x7FFFFFFFu) return refuse("rows x cols out of range");
+  const dim3 grid((uint32_t)((units + per - 1) / per));
   cudaStream_t st = (cudaStream_t)stream;
   if (dtype == FMT_BF16) {
     auto* k = block_rows == 1 ? quantize_kernel<uint16_t, 1> : quantize_kernel<uint16_t, BLOCK>;
-    return launch_result(launch_overlapped(k, grid, dim3(block_rows == 1 ? 128 : 256), 0, st, (const uint16_t*)x_dev, rows, cols, row_stride_elems, q_dev, q_stride,
+    return launch_result(launch_overlapped(k, grid, dim3(QUANTIZE_WARPS * 32), 0, st, (const uint16_t*)x_dev, rows, cols, row_stride_elems, q_dev, q_stride,
                                            scales_dev, scale_stride));
   }
   auto* k = block_rows == 1 ? quantize_kernel<float, 1> : quantize_kernel<float, BLOCK>;
-  return launch_result(launch_overlapped(k, grid, dim3(block_rows == 1 ? 128 : 256), 0, st, (const float*)x_dev, rows, cols, row_stride_elems, q_dev, q_stride, scales_dev,
+  return launch_result(launch_overlapped(k, grid, dim3(QUANTIZE_WARPS * 32), 0, st, (const float*)x_dev, rows, cols, row_stride_elems, q_dev, q_stride, scales_dev,
                                          scale_stride));
 }
 
