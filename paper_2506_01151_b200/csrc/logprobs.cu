@@ -76,6 +76,7 @@ struct Row {
   __device__ __forceinline__ uint32_t first(uint32_t vector) const { return head + vector * W; }
   __device__ __forceinline__ uint32_t bits(uint32_t vector) const {
     const uint32_t v = first(vector), sh = v & 31u;
+    if (head == 0) return reinterpret_cast<const uint8_t*>(mask)[v >> 3] >> (v & 7u) & ((1u << W) - 1u);  // in one byte
     const uint32_t lo = mask[v >> 5], hi = sh + W > 32u ? mask[(v >> 5) + 1u] : 0u;  // (the vector ends before V: the word is there)
     return __funnelshift_r(lo, hi, sh) & ((1u << W) - 1u);
   }
@@ -122,6 +123,48 @@ __device__ __forceinline__ float largest(const uint4& x, float) {
   return fmaxf(fmaxf(__uint_as_float(x.x), __uint_as_float(x.y)), fmaxf(__uint_as_float(x.z), __uint_as_float(x.w)));
 }
 
+// Two values at a time.
+__device__ __forceinline__ uint64_t two(float lo, float hi) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+  return p;
+}
+__device__ __forceinline__ float lo(uint64_t p) { return __uint_as_float((uint32_t)p); }
+__device__ __forceinline__ float hi(uint64_t p) { return __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// A vector's values in pairs, nothing below LOW (-inf becomes LOW; a NaN stays).  LOW lies so far below a row's largest logit that
+// its probability is 0, and is finite, so that 0 times what is made of it is 0.  This holds for rows whose largest logit is above
+// LOW / 10 and whose temperature is between 2e-6 and 1e8 (`ordinary`): 0.9 x 2^40 x 1e-8 is 9,900 powers of two.  In others
+// every value is looked at.
+constexpr float LOW = -0x1p40f;
+__device__ __forceinline__ bool ordinary(float largest, float c) { return largest > LOW * 0.1f && c > 1e-8f && c < 1e6f; }
+__device__ __forceinline__ uint64_t pair_of(const uint4& x, uint32_t i, uint16_t) {
+  uint32_t w = i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w) : "r"(w), "r"(0xD380D380u));
+  return two(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint64_t pair_of(const uint4& x, uint32_t i, float) {
+  float a = __uint_as_float(i == 0 ? x.x : x.z), b = __uint_as_float(i == 0 ? x.y : x.w);
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(LOW));
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(LOW));
+  return two(a, b);
+}
+
 // ------------------------------------------------------------------------------------------------ sums of a row
 //
 // One pass: s = sum of 2^d and t = sum of 2^d d with d = (x - m) log2(e) / T and m the largest logit so far, rescaled when m grows.
@@ -145,6 +188,29 @@ struct Sums {
     const float d = (x - base) * c, p = ex2(d);
     s += p;
     t = fmaf(p, fmaxf(d, -1024.0f), t);  // (d may be -inf; p is 0 below -1024)
+  }
+  // Vectors whose largest logits m has grown for.
+  template <typename T, uint32_t N>
+  __device__ __forceinline__ void add(const uint4 (&x)[N], float c) {
+    const float b = base();
+    if (ordinary(m, c)) {
+      const uint64_t b2 = two(-b, -b), c2 = two(c, c);
+      uint64_t s2 = two(s, 0.0f), t2 = two(t, 0.0f);
+#pragma unroll
+      for (uint32_t u = 0; u < N; ++u)
+#pragma unroll
+        for (uint32_t e = 0; e < 8u / sizeof(T); ++e) {
+          const uint64_t d = mul2(add2(pair_of(x[u], e, T()), b2), c2), p = two(ex2(lo(d)), ex2(hi(d)));
+          s2 = add2(s2, p);
+          t2 = fma2(p, d, t2);
+        }
+      s = lo(s2) + hi(s2), t = lo(t2) + hi(t2);
+    } else {
+#pragma unroll
+      for (uint32_t u = 0; u < N; ++u)
+#pragma unroll
+        for (uint32_t e = 0; e < 16u / sizeof(T); ++e) add(value(x[u], e, T()), b, c);
+    }
   }
   __device__ __forceinline__ void join(Sums o, float c) {
     const float to = fmaxf(m, o.m);
@@ -174,7 +240,7 @@ __device__ __forceinline__ uint64_t max_key(uint64_t a, uint64_t b) { return a >
 // the n_top groups whose own largest reaches it hold any: their vectors alone are read again (L2), and what reaches the bound is
 // listed and put in order.  A row of 128,256 logits is passed once, and a sixth of it twice for n_top = 20, whatever its order.
 
-constexpr uint32_t THREADS = 512, WARPS = THREADS / 32, UNROLL = 4;
+constexpr uint32_t THREADS = 512, WARPS = THREADS / 32, UNROLL = 4, BACK_UNROLL = 2;
 constexpr uint32_t GROUPS = 128, GROUP = THREADS / GROUPS;
 constexpr uint32_t MAX_CLUSTER = 8;
 constexpr uint32_t SORT = 512;                    // listed logits that are put in order by counting
@@ -319,32 +385,39 @@ __global__ void __launch_bounds__(THREADS, 2) logprobs_kernel(const Rows R, cons
     a.grow(x, c), a.add(x, a.base(), c);
   }
   const uint32_t from = rank * THREADS + tid, step = cluster * THREADS;
+  // The next vectors are on their way, and the bits of those after them, while some are added up.
+  uint4 x[UNROLL], next[UNROLL];
+  uint32_t bits[UNROLL], ahead[UNROLL];
+  auto ask_bits = [&](uint32_t i, uint32_t (&to)[UNROLL]) {
+#pragma unroll
+    for (uint32_t u = 0; u < UNROLL; ++u)
+      to[u] = i + u * step >= row.vectors ? 0u : MASK ? row.bits(i + u * step) : (1u << Row<T>::W) - 1u;
+  };
+  auto ask = [&](uint32_t i, const uint32_t (&want)[UNROLL], uint4 (&to)[UNROLL]) {
+#pragma unroll
+    for (uint32_t u = 0; u < UNROLL; ++u) to[u] = want[u] ? row.load(i + u * step) : all_forbidden<T>();
+  };
+  ask_bits(from, bits);
+  ask(from, bits, x);
+  ask_bits(from + UNROLL * step, ahead);
   for (uint32_t i = from; i < row.vectors; i += UNROLL * step) {
-    uint4 x[UNROLL];
-    uint32_t bits[UNROLL];
-#pragma unroll
-    for (uint32_t u = 0; u < UNROLL; ++u) {
-      const bool in = u == 0 || i + u * step < row.vectors;
-      bits[u] = !in ? 0u : MASK ? row.bits(i + u * step) : (1u << Row<T>::W) - 1u;
-    }
-#pragma unroll
-    for (uint32_t u = 0; u < UNROLL; ++u) x[u] = bits[u] ? row.load(i + u * step) : all_forbidden<T>();
+    ask(i + UNROLL * step, ahead, next);
     float m = a.m;
 #pragma unroll
     for (uint32_t u = 0; u < UNROLL; ++u) {
       if (MASK) forbid(x[u], bits[u], T());
+      bits[u] = ahead[u];
       const float most = largest(x[u], T());
       if (most > m) {
         m = most;
         if (TOP) where = i + u * step;
       }
     }
+    ask_bits(i + 2u * UNROLL * step, ahead);
     a.grow(m, c);
-    const float base = a.base();
+    a.template add<T, UNROLL>(x, c);
 #pragma unroll
-    for (uint32_t u = 0; u < UNROLL; ++u)
-#pragma unroll
-      for (uint32_t e = 0; e < Row<T>::W; ++e) a.add(value(x[u], e, T()), base, c);
+    for (uint32_t u = 0; u < UNROLL; ++u) x[u] = next[u];
   }
   if (tid < edges && row.edge(tid) >= row.head) {
     const float x = row.at(row.edge(tid));
@@ -484,48 +557,70 @@ __global__ void __launch_bounds__(THREADS) logprobs_backward_kernel(const Rows R
     const float lp2 = fmaf(x - most, c, -log2s), p = exp2f(lp2);
     return x == -INF ? 0.0f : p * fmaf(B, fmaxf(lp2, -1024.0f), A);
   };
-  auto given = [&](uint32_t v) {
+  if (rank == 0 && tid < row.edges) {
+    const uint32_t v = row.edge(tid);
     float sum = 0.0f;
     for (uint32_t k = 0; k < n_tokens; ++k)
       if (tok[k] == (int32_t)v) sum += g[k];
-    return sum * inv;
-  };
-  if (rank == 0 && tid < row.edges) {
-    const uint32_t v = row.edge(tid);
-    put(out + v, grad(row.at(v)) + given(v));
+    put(out + v, grad(row.at(v)) + sum * inv);
   }
-  for (uint32_t i = rank * THREADS + tid; i < row.vectors; i += cluster * THREADS) {
-    const uint32_t bits = MASK ? row.bits(i) : (1u << Row<T>::W) - 1u, v = row.first(i);
-    float y[Row<T>::W];
+  // p = q^2 with q = 2^(lp2 / 2): in range whenever p is, denormal or not
+  const bool is_ordinary = ordinary(most, c);
+  const uint64_t most2 = two(-most, -most), c2 = two(0.5f * c, 0.5f * c), log2s2 = two(-0.5f * log2s, -0.5f * log2s), A2 = two(A, A), B2 = two(2.0f * B, 2.0f * B);
+  const uint32_t step = cluster * THREADS;
+  for (uint32_t base = rank * THREADS + tid; base < row.vectors; base += BACK_UNROLL * step) {
+    uint32_t bits[BACK_UNROLL];
+    uint4 x[BACK_UNROLL];
 #pragma unroll
-    for (uint32_t e = 0; e < Row<T>::W; ++e) y[e] = 0.0f;
-    if (bits) {
-      uint4 x = row.load(i);
-      if (MASK) forbid(x, bits, T());
-#pragma unroll
-      for (uint32_t e = 0; e < Row<T>::W; ++e) y[e] = grad(value(x, e, T()));
-      for (uint32_t k = 0; k < n_tokens; ++k)
-        if ((uint32_t)tok[k] - v < Row<T>::W) {
-#pragma unroll
-          for (uint32_t e = 0; e < Row<T>::W; ++e)
-            if (tok[k] == (int32_t)(v + e)) y[e] = fmaf(g[k], inv, y[e]);
-        }
+    for (uint32_t u = 0; u < BACK_UNROLL; ++u) {
+      const uint32_t i = base + u * step;
+      bits[u] = i >= row.vectors ? 0u : MASK ? row.bits(i) : (1u << Row<T>::W) - 1u;
     }
-    if (aligned) {
-      uint4 w;
-      if constexpr (sizeof(T) == 2) {
-        auto pair = [](float lo, float hi) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-          return *reinterpret_cast<const uint32_t*>(&b);
-        };
-        w = make_uint4(pair(y[0], y[1]), pair(y[2], y[3]), pair(y[4], y[5]), pair(y[6], y[7]));
-      } else {
-        w = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
-      }
-      *reinterpret_cast<uint4*>(out + v) = w;
-    } else {
 #pragma unroll
-      for (uint32_t e = 0; e < Row<T>::W; ++e) put(out + v + e, y[e]);
+    for (uint32_t u = 0; u < BACK_UNROLL; ++u) x[u] = bits[u] ? row.load(base + u * step) : all_forbidden<T>();
+#pragma unroll
+    for (uint32_t u = 0; u < BACK_UNROLL; ++u) {
+      const uint32_t i = base + u * step, v = row.first(i);
+      if (i >= row.vectors) break;
+      uint64_t y[Row<T>::W / 2];
+#pragma unroll
+      for (uint32_t e = 0; e < Row<T>::W / 2; ++e) y[e] = 0;
+      if (bits[u]) {
+        if (MASK) forbid(x[u], bits[u], T());
+        if (is_ordinary) {
+#pragma unroll
+          for (uint32_t e = 0; e < Row<T>::W / 2; ++e) {
+            const uint64_t half = fma2(add2(pair_of(x[u], e, T()), most2), c2, log2s2), q = two(ex2(lo(half)), ex2(hi(half)));
+            y[e] = mul2(mul2(q, q), fma2(B2, half, A2));
+          }
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < Row<T>::W / 2; ++e) y[e] = two(grad(value(x[u], 2 * e, T())), grad(value(x[u], 2 * e + 1, T())));
+        }
+        for (uint32_t k = 0; k < n_tokens; ++k)
+          if ((uint32_t)tok[k] - v < Row<T>::W) {
+            const float add = g[k] * inv;
+#pragma unroll
+            for (uint32_t e = 0; e < Row<T>::W / 2; ++e)
+              y[e] = add2(y[e], two(tok[k] == (int32_t)(v + 2 * e) ? add : 0.0f, tok[k] == (int32_t)(v + 2 * e + 1) ? add : 0.0f));
+          }
+      }
+      if (aligned) {
+        uint4 w;
+        if constexpr (sizeof(T) == 2) {
+          auto both = [](uint64_t p) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(lo(p), hi(p));
+            return *reinterpret_cast<const uint32_t*>(&b);
+          };
+          w = make_uint4(both(y[0]), both(y[1]), both(y[2]), both(y[3]));
+        } else {
+          w = make_uint4((uint32_t)y[0], (uint32_t)(y[0] >> 32), (uint32_t)y[1], (uint32_t)(y[1] >> 32));
+        }
+        *reinterpret_cast<uint4*>(out + v) = w;
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < Row<T>::W; ++e) put(out + v + e, e % 2 ? hi(y[e / 2]) : lo(y[e / 2]));
+      }
     }
   }
 }
