@@ -52,75 +52,128 @@ __device__ __forceinline__ float ex2(float x) {  // below 2^-126: 0, which sums 
   return y;
 }
 
-// ------------------------------------------------------------------------------------------------ rows in vectors of 16 bytes
+// ------------------------------------------------------------------------------------------------ rows in units of 32 bytes
 //
-// A row may begin at any address: vectors are counted from its first 16-byte boundary on, and the few logits before it and behind
-// the last whole vector ("edges") are taken one at a time.  A vector's bits of the mask come from one or two of its words.
+// A row may begin at any address: units are counted from its first 32-byte boundary on, and the few logits before it and behind the
+// last whole unit ("edges") are taken one at a time.  A unit has as many logits as a number of the mask has bits (16 of bf16, 8
+// of fp32), and begins `head` bits behind number i: its bits come from numbers i and i + 1.
+
+struct Unit {
+  uint32_t v[8];
+};
+// Loads that are left out leave what was there.
+__device__ __forceinline__ void load_if(bool wanted, const void* p, Unit& u) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %9, 0;\n@p ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n}"
+               : "+r"(u.v[0]), "+r"(u.v[1]), "+r"(u.v[2]), "+r"(u.v[3]), "+r"(u.v[4]), "+r"(u.v[5]), "+r"(u.v[6]), "+r"(u.v[7])
+               : "l"(p), "r"((uint32_t)wanted));
+}
+__device__ __forceinline__ void load_if(bool wanted, const uint16_t* p, uint32_t& x) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.u16 %0, [%1];\n}" : "+r"(x) : "l"(p), "r"((uint32_t)wanted));
+}
+__device__ __forceinline__ void load_if(bool wanted, const uint8_t* p, uint32_t& x) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.u8 %0, [%1];\n}" : "+r"(x) : "l"(p), "r"((uint32_t)wanted));
+}
+__device__ __forceinline__ void store_unit(void* p, const Unit& u) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u.v[0]), "r"(u.v[1]), "r"(u.v[2]), "r"(u.v[3]), "r"(u.v[4]),
+               "r"(u.v[5]), "r"(u.v[6]), "r"(u.v[7])
+               : "memory");
+}
+
+template <size_t SIZE>
+struct MaskNumber;
+template <>
+struct MaskNumber<2> {
+  using type = uint16_t;
+};
+template <>
+struct MaskNumber<4> {
+  using type = uint8_t;
+};
 
 template <typename T>
 struct Row {
-  static constexpr uint32_t W = 16u / sizeof(T);  // logits of a vector
+  static constexpr uint32_t W = 32u / sizeof(T), ALL = (1u << W) - 1u;  // logits of a unit
+  using Number = typename MaskNumber<sizeof(T)>::type;
   const T* x;
   const uint32_t* mask;  // or nullptr
-  uint32_t V, head, vectors, edges;
+  uint32_t V, head, units, edges;
 
   __device__ __forceinline__ Row(const Rows& R, uint32_t row)
       : x(static_cast<const T*>(R.logits) + (size_t)row * R.stride), mask(R.mask ? R.mask + (size_t)row * R.mask_stride : nullptr), V(R.V) {
-    head = min(V, (uint32_t)((0u - (uint32_t)reinterpret_cast<uintptr_t>(x)) & 15u) / (uint32_t)sizeof(T));
-    vectors = (V - head) / W;
-    edges = V - vectors * W;
+    head = min(V, (uint32_t)((0u - (uint32_t)reinterpret_cast<uintptr_t>(x)) & 31u) / (uint32_t)sizeof(T));
+    units = (V - head) / W;
+    edges = V - units * W;
   }
-  __device__ __forceinline__ uint32_t edge(uint32_t i) const { return i < head ? i : i + vectors * W; }
+  __device__ __forceinline__ uint32_t edge(uint32_t i) const { return i < head ? i : i + units * W; }
   __device__ __forceinline__ bool allows(uint32_t v) const { return !mask || (mask[v >> 5] >> (v & 31u)) & 1u; }
   __device__ __forceinline__ float at(uint32_t v) const { return allows(v) ? to_f32(x[v]) : -INF; }  // -inf: not allowed
-  __device__ __forceinline__ uint32_t first(uint32_t vector) const { return head + vector * W; }
-  __device__ __forceinline__ uint32_t bits(uint32_t vector) const {
-    const uint32_t v = first(vector), sh = v & 31u;
-    if (head == 0) return reinterpret_cast<const uint8_t*>(mask)[v >> 3] >> (v & 7u) & ((1u << W) - 1u);  // in one byte
-    const uint32_t lo = mask[v >> 5], hi = sh + W > 32u ? mask[(v >> 5) + 1u] : 0u;  // (the vector ends before V: the word is there)
-    return __funnelshift_r(lo, hi, sh) & ((1u << W) - 1u);
+  __device__ __forceinline__ uint32_t first(uint32_t unit) const { return head + unit * W; }
+  __device__ __forceinline__ uint32_t bits(uint32_t unit, bool wanted = true) const {  // 0 if not wanted
+    const Number* const at = reinterpret_cast<const Number*>(mask) + unit;
+    uint32_t lo = 0u, hi = 0u;
+    load_if(wanted, at, lo);
+    load_if(wanted && head != 0u, at + 1, hi);  // (the unit ends before V: it is there)
+    return (lo | hi << W) >> head & ALL;
   }
-  __device__ __forceinline__ uint4 load(uint32_t vector) const { return *reinterpret_cast<const uint4*>(x + first(vector)); }
+  __device__ __forceinline__ void load(uint32_t unit, Unit& u, bool wanted = true) const { load_if(wanted, x + first(unit), u); }
 };
 
-// What the mask forbids becomes -inf.
-__device__ __forceinline__ uint32_t keep_pair(uint32_t x, uint32_t spread, uint32_t which) {  // bytes of `spread`: 0x80 or 0
-  uint32_t k;
-  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(k) : "r"(spread), "r"(which));  // (selectors 8 and up repeat a byte's highest bit)
-  return (x & k) | (0xFF80FF80u & ~k);
-}
-__device__ __forceinline__ void forbid(uint4& x, uint32_t bits, uint16_t) {
-  const uint32_t lo = ((bits & 15u) * 0x00204081u & 0x01010101u) << 7, hi = ((bits >> 4) * 0x00204081u & 0x01010101u) << 7;
-  x.x = keep_pair(x.x, lo, 0x9988u), x.y = keep_pair(x.y, lo, 0xBBAAu);
-  x.z = keep_pair(x.z, hi, 0x9988u), x.w = keep_pair(x.w, hi, 0xBBAAu);
-}
-__device__ __forceinline__ void forbid(uint4& x, uint32_t bits, float) {
-  x.x = bits & 1u ? x.x : 0xFF800000u, x.y = bits & 2u ? x.y : 0xFF800000u;
-  x.z = bits & 4u ? x.z : 0xFF800000u, x.w = bits & 8u ? x.w : 0xFF800000u;
+// What the mask forbids becomes -inf.  `of` holds, for every value that the bits of half a unit (bf16: 8, fp32: 4) may have, the bits
+// of that half to keep.
+template <typename T>
+struct Keep {
+  static constexpr uint32_t BITS = 16u / sizeof(T);
+  uint4 of[1u << BITS];
+};
+template <typename T>
+__device__ __forceinline__ uint4 keep_of(uint32_t bits) {
+  auto word = [&](uint32_t i) {
+    if (sizeof(T) == 4) return (bits >> i) & 1u ? 0xFFFFFFFFu : 0u;
+    return ((bits >> (2u * i)) & 1u ? 0x0000FFFFu : 0u) | ((bits >> (2u * i + 1u)) & 1u ? 0xFFFF0000u : 0u);
+  };
+  return make_uint4(word(0), word(1), word(2), word(3));
 }
 template <typename T>
-__device__ __forceinline__ uint4 all_forbidden() {
-  const uint32_t n = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-  return make_uint4(n, n, n, n);
+__device__ __forceinline__ void forbid(Unit& x, const uint4& low, const uint4& high) {
+  constexpr uint32_t n = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+  const uint32_t k[8] = {low.x, low.y, low.z, low.w, high.x, high.y, high.z, high.w};
+#pragma unroll
+  for (uint32_t i = 0; i < 8; ++i) x.v[i] = (x.v[i] & k[i]) | (n & ~k[i]);
 }
-__device__ __forceinline__ float value(const uint4& x, uint32_t i, uint16_t) {
-  const uint32_t w = i / 2 == 0 ? x.x : i / 2 == 1 ? x.y : i / 2 == 2 ? x.z : x.w;
-  return __uint_as_float(i % 2 ? w & 0xFFFF0000u : w << 16);
+template <typename T>
+__device__ __forceinline__ void forbid(Unit& x, const Keep<T>& keep, uint32_t bits) {
+  forbid<T>(x, keep.of[bits & ((1u << Keep<T>::BITS) - 1u)], keep.of[bits >> Keep<T>::BITS]);
 }
-__device__ __forceinline__ float value(const uint4& x, uint32_t i, float) {
-  return __uint_as_float(i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w);
+template <typename T>
+__device__ __forceinline__ void forbid(Unit& x, uint32_t bits) {  // the same without a table
+  forbid<T>(x, keep_of<T>(bits & ((1u << Keep<T>::BITS) - 1u)), keep_of<T>(bits >> Keep<T>::BITS));
 }
+__device__ __forceinline__ float value(const Unit& x, uint32_t i, uint16_t) {
+  return __uint_as_float(i % 2 ? x.v[i / 2] & 0xFFFF0000u : x.v[i / 2] << 16);
+}
+__device__ __forceinline__ float value(const Unit& x, uint32_t i, float) { return __uint_as_float(x.v[i]); }
 __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {  // (of a NaN and a number: the number)
   uint32_t m;
   asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
   return m;
 }
-__device__ __forceinline__ float largest(const uint4& x, uint16_t) {
-  const uint32_t m = max_pair(max_pair(x.x, x.y), max_pair(x.z, x.w));
+template <uint32_t N>
+__device__ __forceinline__ float largest(const Unit (&x)[N], uint16_t) {
+  uint32_t m = 0xFF80FF80u;
+#pragma unroll
+  for (uint32_t u = 0; u < N; ++u)
+#pragma unroll
+    for (uint32_t i = 0; i < 8; i += 2) m = max_pair(m, max_pair(x[u].v[i], x[u].v[i + 1]));
   return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
 }
-__device__ __forceinline__ float largest(const uint4& x, float) {
-  return fmaxf(fmaxf(__uint_as_float(x.x), __uint_as_float(x.y)), fmaxf(__uint_as_float(x.z), __uint_as_float(x.w)));
+template <uint32_t N>
+__device__ __forceinline__ float largest(const Unit (&x)[N], float) {
+  float m = -INF;
+#pragma unroll
+  for (uint32_t u = 0; u < N; ++u)
+#pragma unroll
+    for (uint32_t i = 0; i < 8; i += 2) m = fmaxf(m, fmaxf(__uint_as_float(x[u].v[i]), __uint_as_float(x[u].v[i + 1])));
+  return m;
 }
 
 // Two values at a time.
@@ -147,22 +200,58 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-// A vector's values in pairs, nothing below LOW (-inf becomes LOW; a NaN stays).  LOW lies so far below a row's largest logit that
+// A unit's values in pairs, nothing below LOW (-inf becomes LOW; a NaN stays).  LOW lies so far below a row's largest logit that
 // its probability is 0, and is finite, so that 0 times what is made of it is 0.  This holds for rows whose largest logit is above
 // LOW / 10 and whose temperature is between 2e-6 and 1e8 (`ordinary`): 0.9 x 2^40 x 1e-8 is 9,900 powers of two.  In others
 // every value is looked at.
 constexpr float LOW = -0x1p40f;
 __device__ __forceinline__ bool ordinary(float largest, float c) { return largest > LOW * 0.1f && c > 1e-8f && c < 1e6f; }
-__device__ __forceinline__ uint64_t pair_of(const uint4& x, uint32_t i, uint16_t) {
-  uint32_t w = i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
-  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w) : "r"(w), "r"(0xD380D380u));
+__device__ __forceinline__ uint64_t pair_of(const Unit& x, uint32_t i, uint16_t) {
+  uint32_t w;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w) : "r"(x.v[i]), "r"(0xD380D380u));
   return two(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
-__device__ __forceinline__ uint64_t pair_of(const uint4& x, uint32_t i, float) {
-  float a = __uint_as_float(i == 0 ? x.x : x.z), b = __uint_as_float(i == 0 ? x.y : x.w);
+__device__ __forceinline__ uint64_t pair_of(const Unit& x, uint32_t i, float) {
+  float a = __uint_as_float(x.v[2 * i]), b = __uint_as_float(x.v[2 * i + 1]);
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(a) : "f"(a), "f"(LOW));
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(b) : "f"(b), "f"(LOW));
   return two(a, b);
+}
+
+// A thread's units from, from + step, ..., N at a time: the next N are on their way, and the bits of those after them, while
+// work(first, units) is at some.  What the mask forbids, and what is behind the row's last unit, is -inf.
+template <typename T, bool MASK, uint32_t N, class F>
+__device__ __forceinline__ void row_turns(const Row<T>& row, uint32_t from, uint32_t step, const Keep<T>& keep, F work) {
+  const uint32_t n = row.units, stride = N * step;
+  auto ask_bits = [&](uint32_t i, uint32_t (&to)[N]) {
+#pragma unroll
+    for (uint32_t u = 0; u < N; ++u) to[u] = MASK ? row.bits(i + u * step, i + u * step < n) : i + u * step < n ? Row<T>::ALL : 0u;
+  };
+  auto ask = [&](uint32_t i, const uint32_t (&bits)[N], Unit (&to)[N]) {
+#pragma unroll
+    for (uint32_t u = 0; u < N; ++u) row.load(i + u * step, to[u], bits[u] != 0u);
+  };
+  Unit xa[N] = {}, xb[N] = {};
+  uint32_t ba[N], bb[N];
+  auto turn = [&](uint32_t i, Unit (&x)[N], uint32_t (&bits)[N], Unit (&next)[N], const uint32_t (&ahead)[N]) {
+    ask(i + stride, ahead, next);
+    if (MASK) {
+#pragma unroll
+      for (uint32_t u = 0; u < N; ++u) forbid(x[u], keep, bits[u]);
+    } else if (i + (N - 1u) * step >= n) {
+#pragma unroll
+      for (uint32_t u = 1; u < N; ++u) forbid<T>(x[u], bits[u]);
+    }
+    ask_bits(i + 2u * stride, bits);
+    work(i, x);
+  };
+  ask_bits(from, ba);
+  ask(from, ba, xa);
+  ask_bits(from + stride, bb);
+  for (uint32_t i = from; i < n; i += 2u * stride) {
+    turn(i, xa, ba, xb, bb);
+    if (i + stride < n) turn(i + stride, xb, bb, xa, ba);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ sums of a row
@@ -189,9 +278,9 @@ struct Sums {
     s += p;
     t = fmaf(p, fmaxf(d, -1024.0f), t);  // (d may be -inf; p is 0 below -1024)
   }
-  // Vectors whose largest logits m has grown for.
+  // Units whose largest logits m has grown for.
   template <typename T, uint32_t N>
-  __device__ __forceinline__ void add(const uint4 (&x)[N], float c) {
+  __device__ __forceinline__ void add(const Unit (&x)[N], float c) {
     const float b = base();
     if (ordinary(m, c)) {
       const uint64_t b2 = two(-b, -b), c2 = two(c, c);
@@ -199,7 +288,7 @@ struct Sums {
 #pragma unroll
       for (uint32_t u = 0; u < N; ++u)
 #pragma unroll
-        for (uint32_t e = 0; e < 8u / sizeof(T); ++e) {
+        for (uint32_t e = 0; e < 16u / sizeof(T); ++e) {
           const uint64_t d = mul2(add2(pair_of(x[u], e, T()), b2), c2), p = two(ex2(lo(d)), ex2(hi(d)));
           s2 = add2(s2, p);
           t2 = fma2(p, d, t2);
@@ -209,13 +298,17 @@ struct Sums {
 #pragma unroll
       for (uint32_t u = 0; u < N; ++u)
 #pragma unroll
-        for (uint32_t e = 0; e < 16u / sizeof(T); ++e) add(value(x[u], e, T()), b, c);
+        for (uint32_t e = 0; e < 32u / sizeof(T); ++e) add(value(x[u], e, T()), b, c);
     }
   }
-  __device__ __forceinline__ void join(Sums o, float c) {
-    const float to = fmaxf(m, o.m);
-    grow(to, c), o.grow(to, c);
-    s += o.s, t += o.t;
+  template <uint32_t LANES>
+  __device__ __forceinline__ void join_lanes(float c) {  // of a warp's first so many lanes, all of which get the result
+    float most = m;
+#pragma unroll
+    for (uint32_t o = LANES / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+    grow(most, c);
+#pragma unroll
+    for (uint32_t o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o), t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
   }
 };
 
@@ -233,22 +326,22 @@ __device__ __forceinline__ uint64_t max_key(uint64_t a, uint64_t b) { return a >
 
 // ------------------------------------------------------------------------------------------------ the forward pass
 //
-// A cluster of 1 to 8 thread blocks to a row; block r takes vectors r * THREADS + thread, and so on in steps of the whole cluster.
+// A cluster of 1 to 8 thread blocks to a row; block r takes units r * THREADS + thread, and so on in steps of the whole cluster.
 //
-// The likeliest tokens.  In the pass over the row each thread keeps the first vector with its largest logit.  The threads make
+// The likeliest tokens.  In the pass over the row each thread keeps the first units with its largest logit.  The threads make
 // 128 groups; of the groups' largest keys (logit, lowest id) the n_top-th is a bound that n_top logits at least reach, and only
-// the n_top groups whose own largest reaches it hold any: their vectors alone are read again (L2), and what reaches the bound is
+// the n_top groups whose own largest reaches it hold any: their units alone are read again (L2), and what reaches the bound is
 // listed and put in order.  A row of 128,256 logits is passed once, and a sixth of it twice for n_top = 20, whatever its order.
 
-constexpr uint32_t THREADS = 512, WARPS = THREADS / 32, UNROLL = 4, BACK_UNROLL = 2;
+constexpr uint32_t THREADS = 256, PER_SM = 4, WARPS = THREADS / 32, UNROLL = 2, BACK_UNROLL = 1;
 constexpr uint32_t GROUPS = 128, GROUP = THREADS / GROUPS;
 constexpr uint32_t MAX_CLUSTER = 8;
-constexpr uint32_t SORT = 512;                    // listed logits that are put in order by counting
-constexpr uint32_t LISTED = SORT + THREADS * 8u;  // what one round of re-reading may add
+constexpr uint32_t SORT = THREADS;                // listed logits that are put in order by counting
+constexpr uint32_t LISTED = SORT + THREADS * 16u;  // what one round of re-reading may add
 
 struct TopShared {
+  alignas(16) uint64_t group[GROUPS];
   uint64_t list[LISTED];
-  uint64_t group[GROUPS];
   uint64_t best[FMT_MAX_TOP];
   uint64_t join[MAX_CLUSTER * FMT_MAX_TOP];  // of the cluster's blocks, in the first one's memory
   uint64_t bound;
@@ -313,20 +406,26 @@ __device__ void find_top(const Row<T>& row, uint32_t from, uint32_t step, uint32
   const uint32_t tid = threadIdx.x;
   for (uint32_t o = 1; o < GROUP; o <<= 1) mine = max_key(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, o));
   if (tid % GROUP == 0) P.group[tid / GROUP] = mine;
-  if (tid == 0) P.n_listed = 0, P.n_chosen = 0, P.bound = 1;
+  if (tid == 0) P.n_listed = 0, P.n_chosen = 0, P.bound = 1, P.best[0] = 0;
   __syncthreads();
   uint32_t above = 0;
   if (tid < GROUPS) {
     mine = P.group[tid];
-    for (uint32_t i = 0; i < GROUPS; ++i) above += P.group[i] > mine;
+#pragma unroll 8
+    for (uint32_t i = 0; i < GROUPS; i += 2) {
+      const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(P.group + i);
+      above += (k.x > mine) + (k.y > mine);
+    }
     if (mine && above < want) {
       P.chosen[atomicAdd(&P.n_chosen, 1u)] = tid;
       if (above == want - 1) P.bound = mine;
+      if (above == 0) P.best[0] = mine;
     }
   }
   __syncthreads();
+  if (want == 1) return;  // the largest of all
   uint64_t bound = P.bound;
-  const uint32_t rounds_of = (row.vectors + step - 1) / step;  // vectors of a thread, at most
+  const uint32_t rounds_of = (row.units + step - 1) / step;  // units of a thread, at most
   const uint32_t items = P.n_chosen * GROUP * rounds_of;
   auto offer = [&](float x, uint32_t v) {
     const uint64_t key = order_key(x, v);
@@ -348,15 +447,13 @@ __device__ void find_top(const Row<T>& row, uint32_t from, uint32_t step, uint32
     const uint32_t item = base + tid;
     if (item < items) {
       const uint32_t rest = item % (GROUP * rounds_of);
-      const uint32_t vector = from - tid + P.chosen[item / (GROUP * rounds_of)] * GROUP + rest % GROUP + rest / GROUP * step;
-      if (vector < row.vectors) {
-        const uint32_t bits = row.mask ? row.bits(vector) : (1u << Row<T>::W) - 1u;
-        if (bits) {
-          uint4 x = row.load(vector);
-          forbid(x, bits, T());
-          if (largest(x, T()) >= key_logit(bound) || bound == 1)
-            for (uint32_t i = 0; i < Row<T>::W; ++i) offer(value(x, i, T()), row.first(vector) + i);
-        }
+      const uint32_t unit = from - tid + P.chosen[item / (GROUP * rounds_of)] * GROUP + rest % GROUP + rest / GROUP * step;
+      if (unit < row.units) {
+        Unit x[1];
+        row.load(unit, x[0]);
+        if (row.mask) forbid<T>(x[0], row.bits(unit));
+        if (largest(x, T()) >= key_logit(bound) || bound == 1)
+          for (uint32_t i = 0; i < Row<T>::W; ++i) offer(value(x[0], i, T()), row.first(unit) + i);
       }
     }
   }
@@ -365,97 +462,80 @@ __device__ void find_top(const Row<T>& row, uint32_t from, uint32_t step, uint32
 }
 
 template <typename T, bool MASK, bool TOP>
-__global__ void __launch_bounds__(THREADS, 2) logprobs_kernel(const Rows R, const Outputs O, const uint32_t cluster) {
+__global__ void __launch_bounds__(THREADS, PER_SM) logprobs_kernel(const Rows R, const Outputs O, const uint32_t cluster) {
   __shared__ JoinShared J;
-  __shared__ __align__(8) uint8_t top_raw[TOP ? sizeof(TopShared) : 8];
+  __shared__ Keep<T> keep;  // (of masked rows)
+  __shared__ __align__(16) uint8_t top_raw[TOP ? sizeof(TopShared) : 16];
   TopShared& P = *reinterpret_cast<TopShared*>(top_raw);
+  const uint32_t tid = threadIdx.x;
   if (cluster > 1) cluster_arrive();
+  if (MASK) {
+    if (tid < sizeof(Keep<T>) / sizeof(uint4)) keep.of[tid] = keep_of<T>(tid);
+    __syncthreads();
+  }
   before_me();
-  const uint32_t tid = threadIdx.x, rank = cluster > 1 ? cluster_rank() : 0u, row_id = blockIdx.x / cluster;
+  const uint32_t rank = cluster > 1 ? cluster_rank() : 0u, row_id = blockIdx.x / cluster;
   const Row<T> row(R, row_id);
   const float temperature = R.temperature ? R.temperature[row_id] : 1.0f;
   const float inv = __fdiv_rn(1.0f, temperature), c = inv * 1.44269504f;  // log2(e)
+  int32_t token = -1;  // (asked for now, wanted at the end)
+  float token_logit = 0.0f;
+  if (rank == 0 && tid < R.n_tokens) {
+    token = R.tokens[(size_t)row_id * R.n_tokens + tid];
+    if (token >= 0 && token < (int64_t)R.V) token_logit = row.at((uint32_t)token);
+  }
 
   Sums a;
-  uint32_t where = 0xFFFFFFFFu;  // the first vector with the thread's largest logit, or, behind all vectors, an edge
+  uint32_t where = 0xFFFFFFFFu;  // the first of the units among which the thread's largest logit is, or, behind all units, an edge
   const uint32_t edges = rank == 0 ? row.edges : 0u;
   if (tid < edges && row.edge(tid) < row.head) {
     const float x = row.at(row.edge(tid));
-    if (x > a.m) where = row.vectors + tid;
+    if (x > a.m) where = row.units + tid;
     a.grow(x, c), a.add(x, a.base(), c);
   }
+
   const uint32_t from = rank * THREADS + tid, step = cluster * THREADS;
-  // The next vectors are on their way, and the bits of those after them, while some are added up.
-  uint4 x[UNROLL], next[UNROLL];
-  uint32_t bits[UNROLL], ahead[UNROLL];
-  auto ask_bits = [&](uint32_t i, uint32_t (&to)[UNROLL]) {
-#pragma unroll
-    for (uint32_t u = 0; u < UNROLL; ++u)
-      to[u] = i + u * step >= row.vectors ? 0u : MASK ? row.bits(i + u * step) : (1u << Row<T>::W) - 1u;
-  };
-  auto ask = [&](uint32_t i, const uint32_t (&want)[UNROLL], uint4 (&to)[UNROLL]) {
-#pragma unroll
-    for (uint32_t u = 0; u < UNROLL; ++u) to[u] = want[u] ? row.load(i + u * step) : all_forbidden<T>();
-  };
-  ask_bits(from, bits);
-  ask(from, bits, x);
-  ask_bits(from + UNROLL * step, ahead);
-  for (uint32_t i = from; i < row.vectors; i += UNROLL * step) {
-    ask(i + UNROLL * step, ahead, next);
-    float m = a.m;
-#pragma unroll
-    for (uint32_t u = 0; u < UNROLL; ++u) {
-      if (MASK) forbid(x[u], bits[u], T());
-      bits[u] = ahead[u];
-      const float most = largest(x[u], T());
-      if (most > m) {
-        m = most;
-        if (TOP) where = i + u * step;
-      }
+  row_turns<T, MASK, UNROLL>(row, from, step, keep, [&](uint32_t i, const Unit (&x)[UNROLL]) {
+    const float most = largest(x, T());
+    if (most > a.m) {
+      if (TOP) where = i;
+      a.grow(most, c);
     }
-    ask_bits(i + 2u * UNROLL * step, ahead);
-    a.grow(m, c);
     a.template add<T, UNROLL>(x, c);
-#pragma unroll
-    for (uint32_t u = 0; u < UNROLL; ++u) x[u] = next[u];
-  }
+  });
   if (tid < edges && row.edge(tid) >= row.head) {
     const float x = row.at(row.edge(tid));
-    if (x > a.m) where = row.vectors + tid;
+    if (x > a.m) where = row.units + tid;
     a.grow(x, c), a.add(x, a.base(), c);
   }
 
   if (TOP) {
     uint64_t mine = 0;
     if (where != 0xFFFFFFFFu) {
-      if (where >= row.vectors) {
-        mine = order_key(a.m, row.edge(where - row.vectors));
+      if (where >= row.units) {
+        mine = order_key(a.m, row.edge(where - row.units));
       } else {
-        uint4 x = row.load(where);
-        forbid(x, MASK ? row.bits(where) : (1u << Row<T>::W) - 1u, T());
-        uint32_t at = 0;
-        for (uint32_t e = Row<T>::W; e-- > 0;)
-          if (value(x, e, T()) == a.m) at = e;
-        mine = order_key(a.m, row.first(where) + at);
+#pragma unroll
+        for (uint32_t u = 0; u < UNROLL; ++u)
+          if (where + u * step < row.units) {
+            Unit x;
+            row.load(where + u * step, x);
+            if (MASK) forbid(x, keep, row.bits(where + u * step));
+#pragma unroll
+            for (uint32_t e = 0; e < Row<T>::W; ++e)
+              if (value(x, e, T()) == a.m) mine = max_key(mine, order_key(a.m, row.first(where + u * step) + e));
+          }
       }
     }
     find_top(row, from, step, edges, mine, O.n_top, P);
   }
 
-  for (uint32_t o = 16; o; o >>= 1) {
-    Sums b;
-    b.m = __shfl_xor_sync(0xFFFFFFFFu, a.m, o), b.s = __shfl_xor_sync(0xFFFFFFFFu, a.s, o), b.t = __shfl_xor_sync(0xFFFFFFFFu, a.t, o);
-    a.join(b, c);
-  }
+  a.join_lanes<32>(c);
   if (tid % 32u == 0) J.warps[tid / 32u] = a;
   __syncthreads();
   if (tid < 32) {
     a = tid < WARPS ? J.warps[tid] : Sums();
-    for (uint32_t o = WARPS / 2; o; o >>= 1) {
-      Sums b;
-      b.m = __shfl_xor_sync(0xFFFFFFFFu, a.m, o), b.s = __shfl_xor_sync(0xFFFFFFFFu, a.s, o), b.t = __shfl_xor_sync(0xFFFFFFFFu, a.t, o);
-      a.join(b, c);
-    }
+    a.join_lanes<WARPS>(c);
   }
   if (cluster > 1) {
     cluster_wait();  // the first block has begun: its memory may be written
@@ -467,9 +547,9 @@ __global__ void __launch_bounds__(THREADS, 2) logprobs_kernel(const Rows R, cons
     cluster_arrive();
     cluster_wait();
     if (rank) return;
-    if (tid == 0) {
-      a = Sums();
-      for (uint32_t i = 0; i < cluster; ++i) a.join(J.blocks[i], c);
+    if (tid < 32) {
+      a = tid < cluster ? J.blocks[tid] : Sums();
+      a.join_lanes<MAX_CLUSTER>(c);
     }
     if (TOP) {
       // the blocks' lists are in order: a key's place is its own in its list and, of every other one, how many are above
@@ -501,12 +581,8 @@ __global__ void __launch_bounds__(THREADS, 2) logprobs_kernel(const Rows R, cons
   const bool bad = a.s != a.s || !(temperature > 0.0f && temperature < INF);
   const float ln = bad ? nan : logf(a.s);  // (-inf of nothing)
   auto logprob = [&](float x) { return bad ? nan : x == -INF ? -INF : (x - a.m) * inv - ln; };
-  bool wrong = false;
-  if (tid < R.n_tokens) {
-    const int32_t v = R.tokens[(size_t)row_id * R.n_tokens + tid];
-    wrong = v < -1 || v >= (int64_t)R.V;
-    if (O.logprobs) O.logprobs[(size_t)row_id * R.n_tokens + tid] = v == -1 ? 0.0f : wrong ? nan : logprob(row.at((uint32_t)v));
-  }
+  const bool wrong = token < -1 || token >= (int64_t)R.V;
+  if (tid < R.n_tokens && O.logprobs) O.logprobs[(size_t)row_id * R.n_tokens + tid] = token == -1 ? 0.0f : wrong ? nan : logprob(token_logit);
   if (TOP && tid < O.n_top) {
     const uint64_t key = P.best[tid];
     const bool there = key && !bad;
@@ -530,11 +606,14 @@ __global__ void __launch_bounds__(THREADS, 2) logprobs_kernel(const Rows R, cons
 // since the gradient may take the logits' place.
 
 template <typename T, bool MASK>
-__global__ void __launch_bounds__(THREADS) logprobs_backward_kernel(const Rows R, const Gradients D, const uint32_t cluster) {
-  before_me();
+__global__ void __launch_bounds__(THREADS, PER_SM) logprobs_backward_kernel(const Rows R, const Gradients D, const uint32_t cluster) {
   __shared__ int32_t tok[FMT_MAX_GIVEN_TOKENS];
   __shared__ float g[FMT_MAX_GIVEN_TOKENS];
-  const uint32_t tid = threadIdx.x, rank = cluster > 1 ? cluster_rank() : 0u, row_id = blockIdx.x / cluster;
+  __shared__ Keep<T> keep;
+  const uint32_t tid = threadIdx.x;
+  if (MASK && tid < sizeof(Keep<T>) / sizeof(uint4)) keep.of[tid] = keep_of<T>(tid);  // (used behind a barrier)
+  before_me();
+  const uint32_t rank = cluster > 1 ? cluster_rank() : 0u, row_id = blockIdx.x / cluster;
   const Row<T> row(R, row_id);
   const float inv = __fdiv_rn(1.0f, R.temperature ? R.temperature[row_id] : 1.0f), c = inv * 1.44269504f;
   const float most = D.norm[2 * (size_t)row_id], ln = D.norm[2 * (size_t)row_id + 1], log2s = ln * 1.44269504f;
@@ -552,83 +631,70 @@ __global__ void __launch_bounds__(THREADS) logprobs_backward_kernel(const Rows R
   for (uint32_t k = 0; k < n_tokens; ++k) total += g[k];
   const float A = -(total + gh * h) * inv, B = gh * -0.693147181f * inv;
   T* const out = static_cast<T*>(D.out) + (size_t)row_id * D.stride;
-  const bool aligned = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.x)) & 15u) == 0;
+  const bool aligned = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.x)) & 31u) == 0;
   auto grad = [&](float x) {
     const float lp2 = fmaf(x - most, c, -log2s), p = exp2f(lp2);
     return x == -INF ? 0.0f : p * fmaf(B, fmaxf(lp2, -1024.0f), A);
   };
   if (rank == 0 && tid < row.edges) {
     const uint32_t v = row.edge(tid);
-    float sum = 0.0f;
+    float d = grad(row.at(v));
     for (uint32_t k = 0; k < n_tokens; ++k)
-      if (tok[k] == (int32_t)v) sum += g[k];
-    put(out + v, grad(row.at(v)) + sum * inv);
+      if (tok[k] == (int32_t)v) d = fmaf(g[k], inv, d);
+    put(out + v, d);
   }
   // p = q^2 with q = 2^(lp2 / 2): in range whenever p is, denormal or not
   const bool is_ordinary = ordinary(most, c);
   const uint64_t most2 = two(-most, -most), c2 = two(0.5f * c, 0.5f * c), log2s2 = two(-0.5f * log2s, -0.5f * log2s), A2 = two(A, A), B2 = two(2.0f * B, 2.0f * B);
   const uint32_t step = cluster * THREADS;
-  for (uint32_t base = rank * THREADS + tid; base < row.vectors; base += BACK_UNROLL * step) {
-    uint32_t bits[BACK_UNROLL];
-    uint4 x[BACK_UNROLL];
+  row_turns<T, MASK, BACK_UNROLL>(row, rank * THREADS + tid, step, keep, [&](uint32_t first, const Unit (&x)[BACK_UNROLL]) {
 #pragma unroll
     for (uint32_t u = 0; u < BACK_UNROLL; ++u) {
-      const uint32_t i = base + u * step;
-      bits[u] = i >= row.vectors ? 0u : MASK ? row.bits(i) : (1u << Row<T>::W) - 1u;
-    }
-#pragma unroll
-    for (uint32_t u = 0; u < BACK_UNROLL; ++u) x[u] = bits[u] ? row.load(base + u * step) : all_forbidden<T>();
-#pragma unroll
-    for (uint32_t u = 0; u < BACK_UNROLL; ++u) {
-      const uint32_t i = base + u * step, v = row.first(i);
-      if (i >= row.vectors) break;
+      const uint32_t i = first + u * step, v = row.first(i);
+      if (i >= row.units) break;
       uint64_t y[Row<T>::W / 2];
+      if (is_ordinary) {
 #pragma unroll
-      for (uint32_t e = 0; e < Row<T>::W / 2; ++e) y[e] = 0;
-      if (bits[u]) {
-        if (MASK) forbid(x[u], bits[u], T());
-        if (is_ordinary) {
-#pragma unroll
-          for (uint32_t e = 0; e < Row<T>::W / 2; ++e) {
-            const uint64_t half = fma2(add2(pair_of(x[u], e, T()), most2), c2, log2s2), q = two(ex2(lo(half)), ex2(hi(half)));
-            y[e] = mul2(mul2(q, q), fma2(B2, half, A2));
-          }
-        } else {
-#pragma unroll
-          for (uint32_t e = 0; e < Row<T>::W / 2; ++e) y[e] = two(grad(value(x[u], 2 * e, T())), grad(value(x[u], 2 * e + 1, T())));
+        for (uint32_t e = 0; e < Row<T>::W / 2; ++e) {
+          const uint64_t half = fma2(add2(pair_of(x[u], e, T()), most2), c2, log2s2), q = two(ex2(lo(half)), ex2(hi(half)));
+          y[e] = mul2(mul2(q, q), fma2(B2, half, A2));
         }
-        for (uint32_t k = 0; k < n_tokens; ++k)
-          if ((uint32_t)tok[k] - v < Row<T>::W) {
-            const float add = g[k] * inv;
+      } else {
 #pragma unroll
-            for (uint32_t e = 0; e < Row<T>::W / 2; ++e)
-              y[e] = add2(y[e], two(tok[k] == (int32_t)(v + 2 * e) ? add : 0.0f, tok[k] == (int32_t)(v + 2 * e + 1) ? add : 0.0f));
-          }
+        for (uint32_t e = 0; e < Row<T>::W / 2; ++e) y[e] = two(grad(value(x[u], 2 * e, T())), grad(value(x[u], 2 * e + 1, T())));
       }
-      if (aligned) {
-        uint4 w;
-        if constexpr (sizeof(T) == 2) {
-          auto both = [](uint64_t p) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(lo(p), hi(p));
-            return *reinterpret_cast<const uint32_t*>(&b);
-          };
-          w = make_uint4(both(y[0]), both(y[1]), both(y[2]), both(y[3]));
-        } else {
-          w = make_uint4((uint32_t)y[0], (uint32_t)(y[0] >> 32), (uint32_t)y[1], (uint32_t)(y[1] >> 32));
+      for (uint32_t k = 0; k < n_tokens; ++k)
+        if ((uint32_t)tok[k] - v < Row<T>::W) {
+          const float add = g[k] * inv;
+#pragma unroll
+          for (uint32_t e = 0; e < Row<T>::W / 2; ++e)
+            y[e] = add2(y[e], two(tok[k] == (int32_t)(v + 2 * e) ? add : 0.0f, tok[k] == (int32_t)(v + 2 * e + 1) ? add : 0.0f));
         }
-        *reinterpret_cast<uint4*>(out + v) = w;
+      if (aligned) {
+        Unit w;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(lo(y[e]), hi(y[e]));
+            w.v[e] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) w.v[e] = (uint32_t)(y[e / 2] >> (e % 2 * 32u));
+        }
+        store_unit(out + v, w);
       } else {
 #pragma unroll
         for (uint32_t e = 0; e < Row<T>::W; ++e) put(out + v + e, e % 2 ? hi(y[e / 2]) : lo(y[e / 2]));
       }
     }
-  }
+  });
 }
 
-// Blocks to a row: as many as fill the GPU (two to an SM), while each has a vector for every thread at least.
+// Blocks to a row: as many as fill the GPU (two to an SM), while each has a unit for every thread at least.
 uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width) {
   uint32_t c = 1;
-  while (c < MAX_CLUSTER && rows * (c * 2u) <= 2u * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
+  while (c < MAX_CLUSTER && rows * (c * 2u) <= PER_SM * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
   return c;
 }
 
@@ -676,7 +742,7 @@ extern "C" fmt_status fmt_token_logprobs(const void* logits_dev, fmt_dtype dtype
                                 top_ids_dev, top_logprobs_dev, status_dev}))
     return s;
   const Outputs O{top_ids_dev || top_logprobs_dev ? n_top : 0u, logprobs_dev, norm_dev, entropy_dev, top_ids_dev, top_logprobs_dev, status_dev};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 8 : 4);
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8);
   void (*k)(Rows, Outputs, uint32_t);
   if (dtype == FMT_BF16)
     k = mask_dev ? O.n_top ? logprobs_kernel<uint16_t, true, true> : logprobs_kernel<uint16_t, true, false>
@@ -706,7 +772,7 @@ extern "C" fmt_status fmt_token_logprobs_backward(const void* logits_dev, fmt_dt
                                 grad_entropy_dev, grad_logits_dev}))
     return s;
   const Gradients D{norm_dev, entropy_dev, grad_logprobs_dev, grad_entropy_dev, grad_logits_dev, grad_stride_elems};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 8 : 4);
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8);
   auto* k = dtype == FMT_BF16 ? mask_dev ? logprobs_backward_kernel<uint16_t, true> : logprobs_backward_kernel<uint16_t, false>
                               : mask_dev ? logprobs_backward_kernel<float, true> : logprobs_backward_kernel<float, false>;
   return launch_result(launch_clusters(k, rows, cluster, (cudaStream_t)stream, R, D, cluster));
