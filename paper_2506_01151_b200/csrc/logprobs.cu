@@ -62,16 +62,20 @@ struct Unit {
   uint32_t v[8];
 };
 // Loads that are left out leave what was there.
-__device__ __forceinline__ void load_if(bool wanted, const void* p, Unit& u) {
+__device__ __forceinline__ void load_if(uint32_t not_zero, const void* p, Unit& u) {
   asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %9, 0;\n@p ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n}"
                : "+r"(u.v[0]), "+r"(u.v[1]), "+r"(u.v[2]), "+r"(u.v[3]), "+r"(u.v[4]), "+r"(u.v[5]), "+r"(u.v[6]), "+r"(u.v[7])
-               : "l"(p), "r"((uint32_t)wanted));
+               : "l"(p), "r"(not_zero));
 }
-__device__ __forceinline__ void load_if(bool wanted, const uint16_t* p, uint32_t& x) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.u16 %0, [%1];\n}" : "+r"(x) : "l"(p), "r"((uint32_t)wanted));
+__device__ __forceinline__ uint32_t load_below(uint32_t i, uint32_t n, const uint16_t* p) {  // 0 unless i < n
+  uint32_t x = 0u;
+  asm volatile("{\n.reg .pred p;\nsetp.lt.u32 p, %2, %3;\n@p ld.global.u16 %0, [%1];\n}" : "+r"(x) : "l"(p), "r"(i), "r"(n));
+  return x;
 }
-__device__ __forceinline__ void load_if(bool wanted, const uint8_t* p, uint32_t& x) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.u8 %0, [%1];\n}" : "+r"(x) : "l"(p), "r"((uint32_t)wanted));
+__device__ __forceinline__ uint32_t load_below(uint32_t i, uint32_t n, const uint8_t* p) {
+  uint32_t x = 0u;
+  asm volatile("{\n.reg .pred p;\nsetp.lt.u32 p, %2, %3;\n@p ld.global.u8 %0, [%1];\n}" : "+r"(x) : "l"(p), "r"(i), "r"(n));
+  return x;
 }
 __device__ __forceinline__ void store_unit(void* p, const Unit& u) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u.v[0]), "r"(u.v[1]), "r"(u.v[2]), "r"(u.v[3]), "r"(u.v[4]),
@@ -108,14 +112,14 @@ struct Row {
   __device__ __forceinline__ bool allows(uint32_t v) const { return !mask || (mask[v >> 5] >> (v & 31u)) & 1u; }
   __device__ __forceinline__ float at(uint32_t v) const { return allows(v) ? to_f32(x[v]) : -INF; }  // -inf: not allowed
   __device__ __forceinline__ uint32_t first(uint32_t unit) const { return head + unit * W; }
-  __device__ __forceinline__ uint32_t bits(uint32_t unit, bool wanted = true) const {  // 0 if not wanted
+  template <bool ALIGNED = false>  // (head is 0)
+  __device__ __forceinline__ uint32_t bits(uint32_t unit) const {  // none behind the last unit
     const Number* const at = reinterpret_cast<const Number*>(mask) + unit;
-    uint32_t lo = 0u, hi = 0u;
-    load_if(wanted, at, lo);
-    load_if(wanted && head != 0u, at + 1, hi);  // (the unit ends before V: it is there)
-    return (lo | hi << W) >> head & ALL;
+    uint32_t b = load_below(unit, units, at);
+    if (!ALIGNED && head) b = (b | load_below(unit, units, at + 1) << W) >> head & ALL;  // (a unit ends before V: it is there)
+    return b;
   }
-  __device__ __forceinline__ void load(uint32_t unit, Unit& u, bool wanted = true) const { load_if(wanted, x + first(unit), u); }
+  __device__ __forceinline__ void load(uint32_t unit, Unit& u, uint32_t not_zero = 1u) const { load_if(not_zero, x + first(unit), u); }
 };
 
 // What the mask forbids becomes -inf.  `of` holds, for every value that the bits of half a unit (bf16: 8, fp32: 4) may have, the bits
@@ -220,16 +224,16 @@ __device__ __forceinline__ uint64_t pair_of(const Unit& x, uint32_t i, float) {
 
 // A thread's units from, from + step, ..., N at a time: the next N are on their way, and the bits of those after them, while
 // work(first, units) is at some.  What the mask forbids, and what is behind the row's last unit, is -inf.
-template <typename T, bool MASK, uint32_t N, class F>
-__device__ __forceinline__ void row_turns(const Row<T>& row, uint32_t from, uint32_t step, const Keep<T>& keep, F work) {
+template <typename T, bool MASK, bool ALIGNED, uint32_t N, class F>
+__device__ __forceinline__ void row_turns_of(const Row<T>& row, uint32_t from, uint32_t step, const Keep<T>& keep, F work) {
   const uint32_t n = row.units, stride = N * step;
   auto ask_bits = [&](uint32_t i, uint32_t (&to)[N]) {
 #pragma unroll
-    for (uint32_t u = 0; u < N; ++u) to[u] = MASK ? row.bits(i + u * step, i + u * step < n) : i + u * step < n ? Row<T>::ALL : 0u;
+    for (uint32_t u = 0; u < N; ++u) to[u] = MASK ? row.template bits<ALIGNED>(i + u * step) : i + u * step < n ? Row<T>::ALL : 0u;
   };
   auto ask = [&](uint32_t i, const uint32_t (&bits)[N], Unit (&to)[N]) {
 #pragma unroll
-    for (uint32_t u = 0; u < N; ++u) row.load(i + u * step, to[u], bits[u] != 0u);
+    for (uint32_t u = 0; u < N; ++u) row.load(i + u * step, to[u], bits[u]);
   };
   Unit xa[N] = {}, xb[N] = {};
   uint32_t ba[N], bb[N];
@@ -252,6 +256,12 @@ __device__ __forceinline__ void row_turns(const Row<T>& row, uint32_t from, uint
     turn(i, xa, ba, xb, bb);
     if (i + stride < n) turn(i + stride, xb, bb, xa, ba);
   }
+}
+
+template <typename T, bool MASK, uint32_t N, class F>
+__device__ __forceinline__ void row_turns(const Row<T>& row, uint32_t from, uint32_t step, const Keep<T>& keep, F work) {
+  if (MASK && row.head == 0) row_turns_of<T, MASK, true, N>(row, from, step, keep, work);
+  else row_turns_of<T, MASK, false, N>(row, from, step, keep, work);
 }
 
 // ------------------------------------------------------------------------------------------------ sums of a row
@@ -401,8 +411,9 @@ __device__ void best_of_list(TopShared& P, uint32_t want) {
   }
 }
 
-template <typename T>
-__device__ void find_top(const Row<T>& row, uint32_t from, uint32_t step, uint32_t edges, uint64_t mine, uint32_t want, TopShared& P) {
+template <typename T, bool MASK>
+__device__ __forceinline__ void find_top(const Row<T>& row, const Keep<T>& keep, uint32_t from, uint32_t step, uint32_t edges, uint64_t mine, uint32_t want,
+                                         TopShared& P) {
   const uint32_t tid = threadIdx.x;
   for (uint32_t o = 1; o < GROUP; o <<= 1) mine = max_key(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, o));
   if (tid % GROUP == 0) P.group[tid / GROUP] = mine;
@@ -427,15 +438,68 @@ __device__ void find_top(const Row<T>& row, uint32_t from, uint32_t step, uint32
   uint64_t bound = P.bound;
   const uint32_t rounds_of = (row.units + step - 1) / step;  // units of a thread, at most
   const uint32_t items = P.n_chosen * GROUP * rounds_of;
+  const uint32_t each = GROUP * rounds_of;
   auto offer = [&](float x, uint32_t v) {
     const uint64_t key = order_key(x, v);
-    if (x > -INF && key >= bound) P.list[atomicAdd(&P.n_listed, 1u)] = key;
+    if (x > -INF && key >= bound) {
+      const uint32_t at = atomicAdd(&P.n_listed, 1u);
+      if (at < LISTED) P.list[at] = key;
+    }
+  };
+  auto unit_of = [&](uint32_t item) {
+    const uint32_t rest = item % each;
+    return item < items ? from - tid + P.chosen[item / each] * GROUP + rest % GROUP + rest / GROUP * step : 0xFFFFFFFFu;
+  };
+  auto reaches = [&](Unit& x, uint32_t bits) {
+    if (MASK) forbid(x, keep, bits);
+    const Unit one[1] = {x};
+    return bits && (largest(one, T()) >= key_logit(bound) || bound == 1);
+  };
+  auto offer_unit = [&](uint32_t unit, const Unit& x) {
+#pragma unroll
+    for (uint32_t i = 0; i < Row<T>::W; ++i) offer(value(x, i, T()), row.first(unit) + i);
   };
   if (tid < edges) offer(row.at(row.edge(tid)), row.edge(tid));
-  for (uint32_t base = 0; base < items; base += THREADS) {
-    if (base) {
+  constexpr uint32_t AT_ONCE = 4;
+  for (uint32_t base = 0; base < items; base += AT_ONCE * THREADS) {
+    Unit x[AT_ONCE];
+    uint32_t unit[AT_ONCE], bits[AT_ONCE];
+#pragma unroll
+    for (uint32_t u = 0; u < AT_ONCE; ++u) {
+      unit[u] = unit_of(base + u * THREADS + tid);
+      row.load(unit[u], x[u], unit[u] < row.units);
+      bits[u] = MASK ? row.bits(unit[u]) : unit[u] < row.units ? Row<T>::ALL : 0u;
+    }
+    uint32_t hits = 0u;
+#pragma unroll
+    for (uint32_t u = 0; u < AT_ONCE; ++u) hits |= reaches(x[u], bits[u]) ? 1u << u : 0u;
+#pragma unroll 1
+    while (hits) {  // (few have one)
+      const uint32_t u = __ffs(hits) - 1u;
+      hits &= hits - 1u;
+      Unit y = x[0];
+      uint32_t at = unit[0];
+#pragma unroll
+      for (uint32_t k = 1; k < AT_ONCE; ++k)
+        if (u == k) y = x[k], at = unit[k];
+      offer_unit(at, y);
+    }
+  }
+  __syncthreads();
+  if (P.n_listed > LISTED) {  // many of the largest logits are in few groups: again, with the list cut down in time
+    __syncthreads();
+    if (tid == 0) P.n_listed = 0;
+    __syncthreads();
+    if (tid < edges) offer(row.at(row.edge(tid)), row.edge(tid));
+    for (uint32_t base = 0; base < items; base += THREADS) {
+      const uint32_t unit = unit_of(base + tid);
+      if (unit < row.units) {
+        Unit x;
+        row.load(unit, x);
+        if (reaches(x, MASK ? row.bits(unit) : Row<T>::ALL)) offer_unit(unit, x);
+      }
       __syncthreads();
-      if (P.n_listed > SORT) {  // only if many of the largest logits are in few groups
+      if (P.n_listed > SORT) {
         best_of_list(P, want);
         if (tid < want) P.list[tid] = P.best[tid];
         if (tid == 0) P.n_listed = want, P.bound = P.best[want - 1];
@@ -444,20 +508,7 @@ __device__ void find_top(const Row<T>& row, uint32_t from, uint32_t step, uint32
       }
       __syncthreads();
     }
-    const uint32_t item = base + tid;
-    if (item < items) {
-      const uint32_t rest = item % (GROUP * rounds_of);
-      const uint32_t unit = from - tid + P.chosen[item / (GROUP * rounds_of)] * GROUP + rest % GROUP + rest / GROUP * step;
-      if (unit < row.units) {
-        Unit x[1];
-        row.load(unit, x[0]);
-        if (row.mask) forbid<T>(x[0], row.bits(unit));
-        if (largest(x, T()) >= key_logit(bound) || bound == 1)
-          for (uint32_t i = 0; i < Row<T>::W; ++i) offer(value(x[0], i, T()), row.first(unit) + i);
-      }
-    }
   }
-  __syncthreads();
   best_of_list(P, want);
 }
 
@@ -515,19 +566,20 @@ __global__ void __launch_bounds__(THREADS, PER_SM) logprobs_kernel(const Rows R,
       if (where >= row.units) {
         mine = order_key(a.m, row.edge(where - row.units));
       } else {
+        uint32_t at = 0xFFFFFFFFu;
 #pragma unroll
-        for (uint32_t u = 0; u < UNROLL; ++u)
-          if (where + u * step < row.units) {
-            Unit x;
-            row.load(where + u * step, x);
-            if (MASK) forbid(x, keep, row.bits(where + u * step));
+        for (uint32_t u = UNROLL; u-- > 0;) {
+          Unit x = {};
+          row.load(where + u * step, x, where + u * step < row.units);
+          if (MASK) forbid(x, keep, row.bits(where + u * step));
 #pragma unroll
-            for (uint32_t e = 0; e < Row<T>::W; ++e)
-              if (value(x, e, T()) == a.m) mine = max_key(mine, order_key(a.m, row.first(where + u * step) + e));
-          }
+          for (uint32_t e = Row<T>::W; e-- > 0;)
+            if (value(x, e, T()) == a.m && where + u * step < row.units) at = u * step * Row<T>::W + e;
+        }
+        mine = order_key(a.m, row.first(where) + at);
       }
     }
-    find_top(row, from, step, edges, mine, O.n_top, P);
+    find_top<T, MASK>(row, keep, from, step, edges, mine, O.n_top, P);
   }
 
   a.join_lanes<32>(c);
