@@ -351,7 +351,7 @@ constexpr uint32_t LISTED = SORT + THREADS * 16u;  // what one round of re-readi
 
 struct TopShared {
   alignas(16) uint64_t group[GROUPS];
-  uint64_t list[LISTED];
+  alignas(16) uint64_t list[LISTED + 8];
   uint64_t best[FMT_MAX_TOP];
   uint64_t join[MAX_CLUSTER * FMT_MAX_TOP];  // of the cluster's blocks, in the first one's memory
   uint64_t bound;
@@ -387,7 +387,13 @@ __device__ void best_of_list(TopShared& P, uint32_t want) {
     if (tid < n) {
       const uint64_t mine = P.list[tid];
       uint32_t above = 0;
-      for (uint32_t i = 0; i < n; ++i) above += P.list[i] > mine;
+      for (uint32_t i = 0; i < n; i += 8) {  // (eight at a time: each is 30 cycles away)
+        ulonglong2 k[4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) k[u] = *reinterpret_cast<const ulonglong2*>(P.list + i + 2 * u);
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) above += (i + 2 * u < n && k[u].x > mine) + (i + 2 * u + 1 < n && k[u].y > mine);
+      }
       if (above < want) P.best[above] = mine;
     }
     __syncthreads();
@@ -610,17 +616,16 @@ __global__ void __launch_bounds__(THREADS, PER_SM) logprobs_kernel(const Rows R,
       __syncthreads();
       if (tid < n && P.join[tid]) {
         const uint64_t mine = P.join[tid];
-        uint32_t above = 0;
-        for (uint32_t b = 0; b < cluster; ++b) {
-          const uint64_t* l = P.join + b * O.n_top;
-          uint32_t lo = 0, hi = O.n_top;
-          while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (l[mid] > mine) lo = mid + 1;
-            else hi = mid;
+        uint32_t above = 0, at[MAX_CLUSTER] = {};  // by halves, in all lists at once
+#pragma unroll
+        for (uint32_t half = FMT_MAX_TOP; half; half /= 2)
+#pragma unroll
+          for (uint32_t b = 0; b < MAX_CLUSTER; ++b) {
+            const uint32_t to = at[b] + half;
+            if (b < cluster && to <= O.n_top && P.join[b * O.n_top + to - 1] > mine) at[b] = to;
           }
-          above += lo;
-        }
+#pragma unroll
+        for (uint32_t b = 0; b < MAX_CLUSTER; ++b) above += at[b];
         if (above < O.n_top) P.best[above] = mine;
       }
     }
@@ -743,10 +748,13 @@ __global__ void __launch_bounds__(THREADS, PER_SM) logprobs_backward_kernel(cons
   });
 }
 
-// Blocks to a row: as many as fill the GPU (two to an SM), while each has a unit for every thread at least.
-uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width) {
+// Blocks to a row: as many as run at a time, while each has a unit for every thread at least.  A block that looks for alternatives
+// spends several microseconds on them however short its part is, so of those there are two to an SM (rows of 50,001 with 5
+// alternatives, 48 of them: 8 blocks a row 14.3 us, 4 12.2, 2 12.1; 64 rows of 128,256 with 20: 18.4, 15.1, 17.0), unless it
+// is for the second block (256 rows of 128,256 with 20: one 34.8, two 32.1, four 38.7).
+uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width, bool top) {
   uint32_t c = 1;
-  while (c < MAX_CLUSTER && rows * (c * 2u) <= PER_SM * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
+  while (c < MAX_CLUSTER && rows * (c * 2u) <= (top && c > 1 ? 2u : PER_SM) * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
   return c;
 }
 
@@ -794,7 +802,7 @@ extern "C" fmt_status fmt_token_logprobs(const void* logits_dev, fmt_dtype dtype
                                 top_ids_dev, top_logprobs_dev, status_dev}))
     return s;
   const Outputs O{top_ids_dev || top_logprobs_dev ? n_top : 0u, logprobs_dev, norm_dev, entropy_dev, top_ids_dev, top_logprobs_dev, status_dev};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8);
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, O.n_top != 0);
   void (*k)(Rows, Outputs, uint32_t);
   if (dtype == FMT_BF16)
     k = mask_dev ? O.n_top ? logprobs_kernel<uint16_t, true, true> : logprobs_kernel<uint16_t, true, false>
@@ -824,7 +832,7 @@ extern "C" fmt_status fmt_token_logprobs_backward(const void* logits_dev, fmt_dt
                                 grad_entropy_dev, grad_logits_dev}))
     return s;
   const Gradients D{norm_dev, entropy_dev, grad_logprobs_dev, grad_entropy_dev, grad_logits_dev, grad_stride_elems};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8);
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, false);
   auto* k = dtype == FMT_BF16 ? mask_dev ? logprobs_backward_kernel<uint16_t, true> : logprobs_backward_kernel<uint16_t, false>
                               : mask_dev ? logprobs_backward_kernel<float, true> : logprobs_backward_kernel<float, false>;
   return launch_result(launch_clusters(k, rows, cluster, (cudaStream_t)stream, R, D, cluster));
