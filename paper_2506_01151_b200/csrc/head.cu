@@ -476,6 +476,8 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
     T* const logits = static_cast<T*>(A.logits);
     float* const own = scales + SCALE_SLOTS * Shape::slot_floats + (warp - 4u) * Shape::own_floats;
     const float minus_inf = -__int_as_float(0x7F800000), nan = __int_as_float(0x7FC00000);
+    const uintptr_t begins = reinterpret_cast<uintptr_t>(logits) | A.row_stride * sizeof(T);  // rows begin at multiples of
+    const bool by_units = (begins & 31u) == 0, by_words = (begins & 3u) == 0;                 // 32 or of four bytes
     for (uint32_t first = 0; first < n_mine; first += LIST) {
       list_slabs(first);
       const uint32_t n_live = S.n_live;
@@ -493,6 +495,16 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
           constexpr uint32_t FACTORS = WIDE ? 4 : DEPTH * COLS / 2;
           const uint32_t count = n_live - g;                 // slabs that are there
           const uint32_t mine = WIDE ? (count > half * 4u ? min(4u, count - half * 4u) : 0u) : quarter < count ? 1u : 0u;
+          // The masks' words are asked for now.  WIDE: a lane is a row, a word for each of its slabs; else lane c holds row c's.
+          constexpr uint32_t WORDS = WIDE ? 4 : 1;
+          const uint32_t r0 = j * ROWS + (WIDE ? quarter * 32u : half * COLS);  // the first of the warp's rows
+          uint32_t word[WORDS];
+#pragma unroll
+          for (uint32_t i = 0; i < WORDS; ++i) {
+            word[i] = 0xFFFFFFFFu;
+            if (A.mask && (WIDE ? i < mine : mine && lane < COLS) && r0 + lane < A.rows)
+              word[i] = __ldg(A.mask + (size_t)(r0 + lane) * A.mask_stride + S.live[g + (WIDE ? half * 4u + i : quarter)]);
+          }
           uint64_t sum[COLS / 2];
 #pragma unroll
           for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = 0;
@@ -547,42 +559,65 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
           }
           const bool failed = S.gave_up != 0u;
           if (WIDE) {
-            // a lane holds 32 tokens of a row for each slab: turned round, 16 tokens at a time, so that a warp writes them side by side
-            constexpr uint32_t TOKENS = TURN * 4 / sizeof(T);  // 16 words of a row
-            const uint32_t r0 = j * ROWS + quarter * 32u, rows_here = r0 < A.rows ? min(32u, A.rows - r0) : 0u;
-            const bool by_words = ((reinterpret_cast<uintptr_t>(logits) | A.row_stride * sizeof(T)) & 3u) == 0;
+            const uint32_t rows_here = r0 < A.rows ? min(32u, A.rows - r0) : 0u;
             uint32_t* const words = reinterpret_cast<uint32_t*>(own);
+            // One slab's code for all four: sums move down a slab's places each time.  (Code that is run once a tile has to be fetched each
+            // time; unrolled, writing a tile took 8,000 cycles of 34,000.)
+#pragma unroll 1
+            for (uint32_t i = 0; i < mine; ++i) {
+              if (!rows_here) break;
+              const uint32_t v0 = S.live[g + half * 4u + i] * SLAB;
+              uint64_t now[SLAB / 2];
+              const uint32_t allowed = word[0];
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-              if (i >= mine || !rows_here) break;
-              const uint32_t s = S.live[g + half * 4u + i];
-              const uint32_t word = !A.mask ? 0xFFFFFFFFu : lane < rows_here ? __ldg(A.mask + (size_t)(r0 + lane) * A.mask_stride + s) : 0u;
+              for (uint32_t c = 0; c < SLAB / 2; ++c) now[c] = sum[c % (COLS / 2)];
+#pragma unroll
+              for (uint32_t c = SLAB / 2; c < COLS / 2; ++c) sum[(c - SLAB / 2) % (COLS / 2)] = sum[c];
+#pragma unroll
+              for (uint32_t k = 1; k < WORDS; ++k) word[k - 1] = word[k];
+              auto masked = [&](uint32_t c) {
+                const float y = failed ? nan : part(now[c / 2], c % 2);
+                return (allowed >> c) & 1u ? y : minus_inf;
+              };
+              auto packed = [&](uint32_t c) {  // word c of the slab's row
+                return sizeof(T) == 4 ? __float_as_uint(masked(c % SLAB)) : two_bf16(masked(2 * c % SLAB), masked((2 * c + 1) % SLAB));
+              };
+              if (by_units && v0 + SLAB <= A.V) {
+                // a lane holds 32 tokens of a row, which are two (bf16) or four units of 32 bytes
+                if (lane < rows_here) {
+                  T* const to = logits + (size_t)(r0 + lane) * A.row_stride + v0;
+#pragma unroll
+                  for (uint32_t q = 0; q < sizeof(T) * SLAB / 4; q += 8)
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(reinterpret_cast<uint32_t*>(to) + q), "r"(packed(q)),
+                                 "r"(packed(q + 1)), "r"(packed(q + 2)), "r"(packed(q + 3)), "r"(packed(q + 4)), "r"(packed(q + 5)), "r"(packed(q + 6)),
+                                 "r"(packed(q + 7))
+                                 : "memory");
+                }
+                continue;
+              }
+              // rows that begin elsewhere: turned round in shared memory, 16 words of a row at a time, so that a warp writes them side by side
+              constexpr uint32_t TOKENS = TURN * 4 / sizeof(T);
 #pragma unroll
               for (uint32_t t = 0; t < SLAB; t += TOKENS) {
-                auto masked = [&](uint32_t c) {
-                  const float y = failed ? nan : part(sum[(i * SLAB + t + c) / 2], c % 2);
-                  return (word >> (t + c)) & 1u ? y : minus_inf;
-                };
 #pragma unroll
-                for (uint32_t c = 0; c < TURN; ++c)
-                  words[lane * (TURN + 1) + c] = sizeof(T) == 4 ? __float_as_uint(masked(c)) : two_bf16(masked(2 * c % TOKENS), masked((2 * c + 1) % TOKENS));
+                for (uint32_t c = 0; c < TURN; ++c) words[lane * (TURN + 1) + c] = packed(t * sizeof(T) / 4 + c);
                 __syncwarp();
                 if (by_words) {
-                  const uint32_t c = lane % TURN, v = s * SLAB + t + c * (4 / sizeof(T));
+                  const uint32_t c = lane % TURN, v = v0 + t + c * (4 / sizeof(T));
                   T* to = logits + (size_t)(r0 + lane / TURN) * A.row_stride + v;
                   const bool all = v + 4 / sizeof(T) <= A.V, some = v < A.V;
 #pragma unroll
-                  for (uint32_t r = lane / TURN; r < 32u; r += 32u / TURN, to += 2 * A.row_stride) {
-                    const uint32_t y = words[r * (TURN + 1) + c];
-                    if (r < rows_here) {
+                  for (uint32_t r = 0; r < 32u; r += 32u / TURN, to += 2 * A.row_stride) {
+                    const uint32_t y = words[(r + lane / TURN) * (TURN + 1) + c];
+                    if (r + lane / TURN < rows_here) {
                       if (all) *reinterpret_cast<uint32_t*>(to) = y;
                       else if (some) *reinterpret_cast<uint16_t*>(to) = (uint16_t)y;
                     }
                   }
-                } else {  // bf16 in rows that begin at any address
-                  const uint32_t v = s * SLAB + t + lane;
+                } else {  // bf16
+                  const uint32_t v = v0 + t + lane;
                   T* to = logits + (size_t)r0 * A.row_stride + v;
-#pragma unroll 8
+#pragma unroll
                   for (uint32_t r = 0; r < 32u; ++r, to += A.row_stride) {
                     const uint16_t y = reinterpret_cast<const uint16_t*>(words + r * (TURN + 1))[lane];
                     if (r < rows_here && v < A.V) *reinterpret_cast<uint16_t*>(to) = y;
@@ -591,19 +626,19 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
                 __syncwarp();
               }
             }
-          } else if (mine) {
-            const uint32_t s = S.live[g + quarter], v = s * SLAB + lane, r0 = j * ROWS + half * COLS;
+          } else if (mine && r0 < A.rows) {
+            const uint32_t v = S.live[g + quarter] * SLAB + lane;
+            T* to = logits + (size_t)r0 * A.row_stride + v;
+#pragma unroll 1
+            for (uint32_t c0 = 0; c0 < COLS && r0 + c0 < A.rows; c0 += 8) {
 #pragma unroll
-            for (uint32_t c0 = 0; c0 < COLS; c0 += CHUNK) {
-              if (r0 + c0 >= A.rows) break;
-              uint32_t word = 0xFFFFFFFFu;  // lane c holds the mask's word of row c
-              if (A.mask && lane < CHUNK && r0 + c0 + lane < A.rows) word = __ldg(A.mask + (size_t)(r0 + c0 + lane) * A.mask_stride + s);
-#pragma unroll
-              for (uint32_t c = 0; c < CHUNK; ++c) {
-                const uint32_t m = __shfl_sync(0xFFFFFFFFu, word, c);
-                const float y = !((m >> lane) & 1u) ? minus_inf : failed ? nan : part(sum[(c0 + c) / 2], c % 2);
-                if (r0 + c0 + c < A.rows && v < A.V) put(logits + (size_t)(r0 + c0 + c) * A.row_stride + v, y);
+              for (uint32_t c = 0; c < 8; ++c, to += A.row_stride) {
+                const uint32_t m = __shfl_sync(0xFFFFFFFFu, word[0], c0 + c);
+                const float y = !((m >> lane) & 1u) ? minus_inf : failed ? nan : part(sum[c / 2], c % 2);
+                if (r0 + c0 + c < A.rows && v < A.V) put(to, y);
               }
+#pragma unroll
+              for (uint32_t c = 4; c < COLS / 2; ++c) sum[c - 4] = sum[c];
             }
           }
         }
