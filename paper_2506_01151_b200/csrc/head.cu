@@ -101,7 +101,10 @@ __global__ void __launch_bounds__(QUANTIZE_WARPS * 32) quantize_kernel(const T* 
 //
 // Few rows (up to 64): the vocabulary is the M side, four slabs to the 128 lanes of tensor memory, and 16, 32 or 64 rows the N
 // side: M is 128 whatever is there, and a decoding step has many tokens and few rows.  More rows: 128 rows are the M side and eight
-// slabs the N side.  A lane is a row then, and one product of scales serves the 32 sums of a slab.
+// slabs the N side.  A lane is a row then, and one product of scales serves the 32 sums of a slab.  More than 128 rows: two blocks
+// on neighbouring SMs work as a pair (cta_group::2) on 256 rows and eight slabs, each with its own 128 rows and half of the slabs in
+// memory.  A block of columns is then 32 KB of shared memory written and read by each SM, where it was 48 KB, and shared memory
+// (128 bytes a cycle) was what the products waited for.
 //
 // Warps: 0 copies weights and 3 hidden states to shared memory (TMA, a ring of stages), 1 issues the products, 2 copies the scales
 // (a ring of their own, as they are needed later), 4 to 11 add up and write.
@@ -113,22 +116,26 @@ constexpr uint32_t ALL_SLABS = 8192;  // of a vocabulary whose masks every block
 constexpr uint32_t ALL_WORDS = 32768; // of the masks then
 constexpr uint32_t SCALE_SLOTS = 8;
 constexpr uint32_t SLAB_BYTES = SLAB * BLOCK;
-constexpr uint32_t WAIT_POLLS = 1u << 20;
+constexpr uint32_t WAIT_POLLS = 1u << 18;  // of 2,900 cycles, the time after which a wait for nothing comes back
 constexpr uint32_t WIDE_ROWS = 128;        // the M side's
 constexpr uint32_t TURN = 16;              // words of a row that a warp turns round in shared memory on their way out
 
-template <uint32_t ROWS, bool WIDE>
+// FEW: rows (at most 64) are the N side.  WIDE: 128 rows are the M side.  PAIR: 256 rows are, 128 in each of two blocks.
+enum HeadForm { FEW, WIDE, PAIR };
+
+template <uint32_t ROWS, HeadForm FORM>
 struct HeadShape {
-  static constexpr uint32_t slabs = WIDE ? 8 : 4;                     // of a tile
-  static constexpr uint32_t columns = WIDE ? slabs * SLAB : ROWS;     // of tensor memory
-  static constexpr uint32_t depth = WIDE ? 1 : 2;                     // blocks of columns that make a stage: each round of waits costs some 400 cycles
-  static constexpr uint32_t stages = WIDE ? 4 : ROWS == 64 ? 4 : 5;
-  static constexpr uint32_t bufs = WIDE ? 2 : 4;                      // of tensor memory, depth x columns each
-  static constexpr uint32_t block_bytes = slabs * SLAB_BYTES + ROWS * BLOCK;
+  static constexpr uint32_t slabs = FORM == FEW ? 4 : 8;                        // of a tile
+  static constexpr uint32_t slabs_here = FORM == PAIR ? 4 : slabs;              // of them in this block's memory
+  static constexpr uint32_t columns = FORM == FEW ? ROWS : slabs * SLAB;        // of tensor memory
+  static constexpr uint32_t depth = FORM == FEW ? 2 : 1;                        // blocks of columns that make a stage: each round of waits costs some 400 cycles
+  static constexpr uint32_t stages = FORM == PAIR ? 6 : FORM == WIDE ? 4 : ROWS == 64 ? 4 : 5;
+  static constexpr uint32_t bufs = FORM == FEW ? 4 : 2;                         // of tensor memory, depth x columns each
+  static constexpr uint32_t block_bytes = slabs_here * SLAB_BYTES + ROWS * BLOCK;
   static constexpr uint32_t stage_bytes = depth * block_bytes;
-  static constexpr uint32_t block_floats = ROWS + slabs;              // scales
+  static constexpr uint32_t block_floats = ROWS + slabs;                        // scales
   static constexpr uint32_t slot_floats = depth * block_floats;
-  static constexpr uint32_t own_floats = WIDE ? 32 * (TURN + 1) : 0;  // of an adding warp
+  static constexpr uint32_t own_floats = FORM == FEW ? 0 : 32 * (TURN + 1);     // of an adding warp
   static constexpr uint32_t smem = 1024 + stages * stage_bytes + (SCALE_SLOTS * slot_floats + ADD_WARPS * own_floats) * 4;
 };
 
@@ -145,8 +152,8 @@ struct HeadArgs {
 };
 
 struct HeadShared {
-  uint64_t full[5], empty[5], sums_full[4], sums_empty[4];
-  uint32_t tmem, n_live, n_dead, issued[4];
+  uint64_t full[6], empty[6], sums_full[4], sums_empty[4], both_empty[4], through;
+  uint32_t tmem, n_live, n_dead, copied[4];  // (copied: stages, by the copying warps of this block and the other one)
   volatile uint32_t gave_up;
   uint32_t bits[ALL_SLABS / 32], upto[ALL_SLABS / 32];
   uint32_t live[LIST], dead[LIST];
@@ -159,20 +166,48 @@ __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
 }
-__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
-}
+template <bool CLUSTER = false>  // (whether the other block of a pair arrives there, too)
 __device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
   uint32_t done;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-               : "=r"(done) : "r"(smem_addr(b)), "r"(parity) : "memory");
+  if (CLUSTER)
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done) : "r"(smem_addr(b)), "r"(parity) : "memory");
+  else
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done) : "r"(smem_addr(b)), "r"(parity) : "memory");
   return done != 0u;
 }
+// The same variable in the memory of the pair's first block (of a block by itself: its own).
+template <HeadForm FORM>
+__device__ __forceinline__ uint32_t at_first(const void* p) {
+  uint32_t a = smem_addr(p);
+  if (FORM == PAIR) asm("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
+  return a;
+}
+template <HeadForm FORM>
+__device__ __forceinline__ void bar_arrive_at(uint32_t addr) {
+  if (FORM == PAIR) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+  else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+template <HeadForm FORM>
+__device__ __forceinline__ void bar_expect_at(uint32_t addr, uint32_t bytes) {
+  if (FORM == PAIR) asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(addr), "r"(bytes) : "memory");
+  else asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(addr), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint32_t pair_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // Waits until the barrier's phase of this parity is over.  False: given up, here or by another warp of the block.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, HeadShared& S) {
-  if (bar_test(b, parity)) return true;
+  if (bar_test<CLUSTER>(b, parity)) return true;
   for (uint32_t i = 0; i < WAIT_POLLS && !S.gave_up; ++i)
-    if (bar_test(b, parity)) return true;
+    if (bar_test<CLUSTER>(b, parity)) return true;
   S.gave_up = 1u;
   return false;
 }
@@ -206,22 +241,40 @@ struct Ring {
   }
 };
 
-__device__ __forceinline__ void tma_load(const CUtensorMap* map, uint64_t* bar, uint32_t dst, uint32_t x, uint32_t y) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map),
-               "r"(smem_addr(bar)), "r"(x), "r"(y)
-               : "memory");
+template <HeadForm FORM>
+__device__ __forceinline__ void tma_load(const CUtensorMap* map, uint32_t bar, uint32_t dst, uint32_t x, uint32_t y) {
+  if (FORM == PAIR)  // (the barrier may be the other block's)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(bar), "r"(x), "r"(y)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map), "r"(bar),
+                 "r"(x), "r"(y)
+                 : "memory");
 }
 // Rows of 128 bytes, swizzled in groups of eight (1,024 bytes), version 1 of the descriptor.
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
+template <HeadForm FORM>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-               "r"((uint32_t)add)
-               : "memory");
+  if (FORM == PAIR)
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                 "r"((uint32_t)add)
+                 : "memory");
+  else
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                 "r"((uint32_t)add)
+                 : "memory");
 }
+// The barrier (in both blocks of a pair) hears when the products issued so far are through.
+template <HeadForm FORM>
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+  if (FORM == PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"((uint16_t)3)
+                 : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 __device__ __forceinline__ void block_sync() { asm volatile("bar.sync 1, %0;" ::"n"(HEAD_THREADS) : "memory"); }  // from wherever a warp is
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -268,49 +321,59 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&b);
 }
 
-template <typename T, uint32_t ROWS, bool WIDE>
+template <typename T, uint32_t ROWS, HeadForm FORM>
 __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap wmap4,
                                                                const __grid_constant__ CUtensorMap xmap, const HeadArgs A) {
-  using Shape = HeadShape<ROWS, WIDE>;
-  constexpr uint32_t SLABS = Shape::slabs, DEPTH = Shape::depth, BUF = DEPTH * Shape::columns, TMEM = Shape::bufs * BUF;
+  using Shape = HeadShape<ROWS, FORM>;
+  constexpr uint32_t SLABS = Shape::slabs, DEPTH = Shape::depth, BUF = DEPTH * Shape::columns, TMEM = Shape::bufs * BUF, BLOCKS = FORM == PAIR ? 2 : 1;
+  constexpr bool LANE_IS_ROW = FORM != FEW;
   extern __shared__ uint8_t raw[];
   __shared__ HeadShared S;
-  const uint32_t tiles_at = (smem_addr(raw) + 1023u) & ~1023u;
+  const uint32_t tiles_at = (smem_addr(raw) + 1023u) & ~1023u;  // (the same in both blocks of a pair)
   float* const scales = reinterpret_cast<float*>(raw + (tiles_at - smem_addr(raw)) + Shape::stages * Shape::stage_bytes);
   const uint32_t tid = threadIdx.x, warp = tid / 32u, lane = tid % 32u;
-  const uint32_t n_slabs = (A.V + SLAB - 1) / SLAB, n_blocks = (A.K + BLOCK - 1) / BLOCK, row_tiles = (A.rows + ROWS - 1) / ROWS;
+  const uint32_t rank = FORM == PAIR ? pair_rank() : 0u;
+  const uint32_t n_slabs = (A.V + SLAB - 1) / SLAB, n_blocks = (A.K + BLOCK - 1) / BLOCK, row_tiles = (A.rows + BLOCKS * ROWS - 1) / (BLOCKS * ROWS);
+  const uint32_t party = blockIdx.x / BLOCKS, parties = gridDim.x / BLOCKS;  // a party is a block or a pair: both blocks have the same slabs
 
   if (tid == 0) {
-    for (uint32_t i = 0; i < Shape::stages; ++i) bar_init(&S.full[i], 2), bar_init(&S.empty[i], 1);
-    for (uint32_t i = 0; i < Shape::bufs; ++i) bar_init(&S.sums_full[i], 2), bar_init(&S.sums_empty[i], ADD_WARPS);
-    S.gave_up = 0u, S.issued[0] = S.issued[1] = S.issued[2] = S.issued[3] = 0u;
+    for (uint32_t i = 0; i < Shape::stages; ++i) bar_init(&S.full[i], 2 * BLOCKS), bar_init(&S.empty[i], 1);
+    for (uint32_t i = 0; i < Shape::bufs; ++i) bar_init(&S.sums_full[i], 2), bar_init(&S.sums_empty[i], ADD_WARPS), bar_init(&S.both_empty[i], 2 * ADD_WARPS);
+    bar_init(&S.through, 1);
+    S.gave_up = 0u, S.copied[0] = S.copied[1] = S.copied[2] = S.copied[3] = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&S.tmem)), "n"(TMEM) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (FORM == PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&S.tmem)), "n"(TMEM) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&S.tmem)), "n"(TMEM) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   before_sync();
   __syncthreads();
+  if (FORM == PAIR) pair_sync();  // the other block's barriers are there
   after_sync();
   before_me();
 
   Ring<Shape::stages> stage;
   Ring<Shape::bufs> buf;
   Ring<SCALE_SLOTS> slot;
-  uint32_t issued = 0;  // stages filled (warps 0 and 3) or used (warp 1)
+  uint32_t copied = 0;  // stages, by this thread
   bool failed = false;
 
   // n things are dealt out four at a time, as long as there are four for every block (`fours` times), and then one by one
-  auto share = [&](uint32_t n, uint32_t fours) { return 4u * fours + (n - 4u * fours * gridDim.x + gridDim.x - 1u - blockIdx.x) / gridDim.x; };
+  auto share = [&](uint32_t n, uint32_t fours) { return 4u * fours + (n - 4u * fours * parties + parties - 1u - party) / parties; };
   auto place = [&](uint32_t i, uint32_t fours) {  // of the block's i-th
-    return i < 4u * fours ? 4u * (i / 4u * gridDim.x + blockIdx.x) + i % 4u : i * gridDim.x + blockIdx.x;
+    return i < 4u * fours ? 4u * (i / 4u * parties + party) + i % 4u : i * parties + party;
   };
-  const uint32_t fours = n_slabs / (4u * gridDim.x), n_mine = share(n_slabs, fours);
+  const uint32_t fours = n_slabs / (4u * parties), n_mine = share(n_slabs, fours);
   auto slab_no = [&](uint32_t i) { return place(i, fours); };
   // Small masks are looked at as a whole by every block, and what is left of the vocabulary is dealt out anew: where a grammar leaves
   // few tokens, a block's own slabs have five or six of them, or none (8 rows of 32,000 x 4,096: 19.2 us, so 13.4).
-  const bool whole = A.mask && n_slabs <= ALL_SLABS && (uint64_t)n_slabs * A.rows <= ALL_WORDS && n_slabs > gridDim.x && n_mine < LIST;
+  const bool whole = A.mask && n_slabs <= ALL_SLABS && (uint64_t)n_slabs * A.rows <= ALL_WORDS && n_slabs > parties && n_mine < LIST;
   // The block's slabs from the first-th on that some row may use, and the others.  All threads.
   auto list_slabs = [&](uint32_t first) {
     if (whole) {
@@ -340,7 +403,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
           seen = __shfl_sync(0xFFFFFFFFu, upto, 31);
         }
         __syncwarp();
-        const uint32_t by_four = seen / (4u * gridDim.x), n_live = share(seen, by_four);
+        const uint32_t by_four = seen / (4u * parties), n_live = share(seen, by_four);
         for (uint32_t k = lane; k < n_live; k += 32) {
           const uint32_t no = place(k, by_four);  // among those
           uint32_t lo = 0, hi = (n_slabs + 31u) / 32u - 1u;
@@ -395,21 +458,23 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
   };
 
   if (warp < 4) {
-    if (WIDE) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // 384 threads of 168 registers: 256 x 216 + 128 x 72 are no more
+    if (LANE_IS_ROW) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // 384 threads of 168 registers: 256 x 216 + 128 x 72 are no more
     for (uint32_t first = 0; first < n_mine; first += LIST) {
       list_slabs(first);
       const uint32_t n_live = S.n_live;
       if (warp == 0 && elected()) {
         for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
           for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
-            const uint32_t count = min(SLABS, n_live - g);
-            uint32_t y[SLABS / 4], whole = 0u;  // of four slabs: the first one's rows, whether the others follow
+            // this block's slabs of the tile: all, or the first or second half of them
+            const uint32_t there = min(SLABS, n_live - g), half = (there + 1u) / 2u, from = FORM == PAIR ? g + rank * half : g;
+            const uint32_t count = FORM == PAIR ? (rank ? there - half : half) : there;
+            uint32_t y[Shape::slabs_here / 4], whole = 0u;  // of four slabs: the first one's rows, whether the others follow
 #pragma unroll
-            for (uint32_t i = 0; i < SLABS / 4; ++i) {
+            for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
               y[i] = 0u;
               if (4u * i + 3u < count) {
-                y[i] = S.live[g + 4u * i] * SLAB;
-                if (S.live[g + 4u * i + 3u] * SLAB == y[i] + 3u * SLAB) whole |= 1u << i;
+                y[i] = S.live[from + 4u * i] * SLAB;
+                if (S.live[from + 4u * i + 3u] * SLAB == y[i] + 3u * SLAB) whole |= 1u << i;
               }
             }
             for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
@@ -417,19 +482,19 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
                 failed = true;
                 break;
               }
-              const uint32_t blocks = min(DEPTH, n_blocks - b);
+              const uint32_t blocks = min(DEPTH, n_blocks - b), bar = at_first<FORM>(&S.full[stage.at]);
               uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
-              uint64_t* bar = &S.full[stage.at];
-              bar_expect(bar, blocks * count * SLAB_BYTES);
+              if (FORM != PAIR || count) bar_expect_at<FORM>(bar, blocks * count * SLAB_BYTES);
+              else bar_arrive_at<FORM>(bar);
               for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) {
 #pragma unroll
-                for (uint32_t i = 0; i < SLABS / 4; ++i) {
-                  if ((whole >> i) & 1u) tma_load(&wmap4, bar, at + 4u * i * SLAB_BYTES, k * BLOCK, y[i]);
+                for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
+                  if ((whole >> i) & 1u) tma_load<FORM>(&wmap4, bar, at + 4u * i * SLAB_BYTES, k * BLOCK, y[i]);
                   else
-                    for (uint32_t q = 4u * i; q < min(4u * i + 4u, count); ++q) tma_load(&wmap, bar, at + q * SLAB_BYTES, k * BLOCK, S.live[g + q] * SLAB);
+                    for (uint32_t q = 4u * i; q < min(4u * i + 4u, count); ++q) tma_load<FORM>(&wmap, bar, at + q * SLAB_BYTES, k * BLOCK, S.live[from + q] * SLAB);
                 }
               }
-              ++issued;
+              ++copied;
               stage.next();
             }
           }
@@ -441,39 +506,39 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
                 failed = true;
                 break;
               }
-              const uint32_t blocks = min(DEPTH, n_blocks - b);
-              uint32_t at = tiles_at + stage.at * Shape::stage_bytes + SLABS * SLAB_BYTES;
-              bar_expect(&S.full[stage.at], blocks * ROWS * BLOCK);
-              for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) tma_load(&xmap, &S.full[stage.at], at, k * BLOCK, j * ROWS);
-              ++issued;
+              const uint32_t blocks = min(DEPTH, n_blocks - b), bar = at_first<FORM>(&S.full[stage.at]);
+              uint32_t at = tiles_at + stage.at * Shape::stage_bytes + Shape::slabs_here * SLAB_BYTES;
+              bar_expect_at<FORM>(bar, blocks * ROWS * BLOCK);
+              for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) tma_load<FORM>(&xmap, bar, at, k * BLOCK, (j * BLOCKS + rank) * ROWS);
+              ++copied;
               stage.next();
             }
-      } else if (warp == 1 && elected()) {
+      } else if (warp == 1 && rank == 0 && elected()) {  // (a pair's products are issued by its first block, for both)
         for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
           for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
-            // e4m3 x e4m3 into fp32, both K-major, 128 lanes
-            const uint32_t columns = WIDE ? min(SLABS, n_live - g) * SLAB : ROWS;
-            const uint32_t idesc = 1u << 4 | (columns >> 3) << 17 | (128u >> 4) << 24;
+            // e4m3 x e4m3 into fp32, both K-major, 128 lanes (of each block)
+            const uint32_t there = min(SLABS, n_live - g), columns = FORM == FEW ? ROWS : FORM == WIDE ? there * SLAB : (there + 1u) / 2u * 2u * SLAB;
+            const uint32_t idesc = 1u << 4 | (columns >> 3) << 17 | (BLOCKS * 128u >> 4) << 24;
             for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
-              if (!bar_wait(&S.sums_empty[buf.at], buf.round ^ 1u, S) || !bar_wait(&S.full[stage.at], stage.round, S)) {
+              if (!bar_wait<FORM == PAIR>(FORM == PAIR ? &S.both_empty[buf.at] : &S.sums_empty[buf.at], buf.round ^ 1u, S) ||
+                  !bar_wait<FORM == PAIR>(&S.full[stage.at], stage.round, S)) {
                 failed = true;
                 break;
               }
               after_sync();
               const uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
-              const uint64_t w = tile_desc(at), x = tile_desc(at + SLABS * SLAB_BYTES);
+              const uint64_t w = tile_desc(at), x = tile_desc(at + Shape::slabs_here * SLAB_BYTES);
 #pragma unroll
               for (uint32_t k = 0; k < DEPTH; ++k)
                 if (k == 0 || b + k < n_blocks) {
 #pragma unroll
                   for (uint32_t i = 0; i < 4; ++i) {
                     const uint32_t more = (k * Shape::block_bytes + 32u * i) >> 4;
-                    mma(S.tmem + buf.at * BUF + k * Shape::columns, (WIDE ? x : w) + more, (WIDE ? w : x) + more, idesc, i != 0);
+                    mma<FORM>(S.tmem + buf.at * BUF + k * Shape::columns, (LANE_IS_ROW ? x : w) + more, (LANE_IS_ROW ? w : x) + more, idesc, i != 0);
                   }
                 }
-              mma_commit(&S.empty[stage.at]);
-              mma_commit(&S.sums_full[buf.at]);
-              ++issued;
+              mma_commit<FORM>(&S.empty[stage.at]);
+              mma_commit<FORM>(&S.sums_full[buf.at]);
               stage.next(), buf.next();
             }
           }
@@ -485,7 +550,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
         for (uint32_t t = 0; t < total + AHEAD; ++t) {
           if (t >= AHEAD) bar_wait_on(&S.sums_empty[buf.at], buf.round ^ 1u, S);
           if (t < total) {
-            const uint32_t count = min(SLABS, n_live - g), r0 = j * ROWS;
+            const uint32_t count = min(SLABS, n_live - g), r0 = (j * BLOCKS + rank) * ROWS;
             for (uint32_t k = b; k < min(b + DEPTH, n_blocks); ++k) {
               const uint32_t dst = smem_addr(scales + slot.at * Shape::slot_floats + (k - b) * Shape::block_floats);
               const float* xp = A.xs + (size_t)k * A.xs_stride + r0;
@@ -517,19 +582,12 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
       __syncwarp();
       block_sync();  // the lists are made anew
     }
-    // nothing of this block's is in flight when it ends: every copy has landed and every product is through
-    if (issued) S.issued[warp] = issued;  // (the threads that were elected)
+    if (warp == 1 && rank == 0 && elected()) mma_commit<FORM>(&S.through);
+    if ((warp == 0 || warp == 3) && copied)  // (the thread that was elected)
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at_first<FORM>(&S.copied[rank * 2u + (warp ? 1u : 0u)])), "r"(copied) : "memory");
     __syncwarp();
-    asm volatile("bar.sync 2, 128;" ::: "memory");
-    if (warp == 0 && lane == 0) {
-      const uint32_t some = min(S.issued[0], S.issued[3]), most = max(S.issued[0], S.issued[3]);
-      for (uint32_t i = some; i < most; ++i) bar_arrive(&S.full[i % Shape::stages]);  // stages that only one of the two copying threads came to fill
-      for (uint32_t i = most - min(most, Shape::stages); i < most; ++i) bar_drain(&S.full[i % Shape::stages], i / Shape::stages & 1u);
-    }
-    if (warp == 1 && lane == 0)
-      for (uint32_t i = S.issued[1] - min(S.issued[1], Shape::stages); i < S.issued[1]; ++i) bar_drain(&S.empty[i % Shape::stages], i / Shape::stages & 1u);
   } else {
-    if (WIDE) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    if (LANE_IS_ROW) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const uint32_t quarter = warp % 4u, half = (warp - 4u) / 4u;  // 32 lanes of tensor memory, half of the columns
     T* const logits = static_cast<T*>(A.logits);
     float* const own = scales + SCALE_SLOTS * Shape::slot_floats + (warp - 4u) * Shape::own_floats;
@@ -543,25 +601,25 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
       for (uint32_t i = warp - 4u; i < S.n_dead; i += ADD_WARPS) {
         const uint32_t v = S.dead[i] * SLAB + lane;
         if (v < A.V)
-          for (uint32_t r = blockIdx.y; r < A.rows; r += gridDim.y) put(logits + (size_t)r * A.row_stride + v, minus_inf);
+          for (uint32_t r = blockIdx.y * BLOCKS + rank; r < A.rows; r += gridDim.y * BLOCKS) put(logits + (size_t)r * A.row_stride + v, minus_inf);
       }
       for (uint32_t g = 0; g < n_live; g += SLABS)
         for (uint32_t j = blockIdx.y; j < row_tiles; j += gridDim.y) {
           constexpr uint32_t COLS = Shape::columns / 2;      // of the tile, this warp's
           constexpr uint32_t CHUNK = COLS < 32 ? COLS : 32;  // read from tensor memory in one go
           constexpr uint32_t READS = DEPTH * COLS / CHUNK;   // of a stage; an even number
-          constexpr uint32_t FACTORS = WIDE ? 4 : DEPTH * COLS / 2;
+          constexpr uint32_t FACTORS = LANE_IS_ROW ? 4 : DEPTH * COLS / 2;
           const uint32_t count = n_live - g;                 // slabs that are there
-          const uint32_t mine = WIDE ? (count > half * 4u ? min(4u, count - half * 4u) : 0u) : quarter < count ? 1u : 0u;
-          // The masks' words are asked for now.  WIDE: a lane is a row, a word for each of its slabs; else lane c holds row c's.
-          constexpr uint32_t WORDS = WIDE ? 4 : 1;
-          const uint32_t r0 = j * ROWS + (WIDE ? quarter * 32u : half * COLS);  // the first of the warp's rows
+          const uint32_t mine = LANE_IS_ROW ? (count > half * 4u ? min(4u, count - half * 4u) : 0u) : quarter < count ? 1u : 0u;
+          // The masks' words are asked for now.  Where a lane is a row, a word for each of its slabs; else lane c holds row c's.
+          constexpr uint32_t WORDS = LANE_IS_ROW ? 4 : 1;
+          const uint32_t r0 = (j * BLOCKS + rank) * ROWS + (LANE_IS_ROW ? quarter * 32u : half * COLS);  // the first of the warp's rows
           uint32_t word[WORDS];
 #pragma unroll
           for (uint32_t i = 0; i < WORDS; ++i) {
             word[i] = 0xFFFFFFFFu;
-            if (A.mask && (WIDE ? i < mine : mine && lane < COLS) && r0 + lane < A.rows)
-              word[i] = __ldg(A.mask + (size_t)(r0 + lane) * A.mask_stride + S.live[g + (WIDE ? half * 4u + i : quarter)]);
+            if (A.mask && (LANE_IS_ROW ? i < mine : mine && lane < COLS) && r0 + lane < A.rows)
+              word[i] = __ldg(A.mask + (size_t)(r0 + lane) * A.mask_stride + S.live[g + (LANE_IS_ROW ? half * 4u + i : quarter)]);
           }
           uint64_t sum[COLS / 2];
 #pragma unroll
@@ -579,7 +637,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
           for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
             uint64_t by[FACTORS];  // the products of two scales
             const float* sc = scales + slot.at * Shape::slot_floats;
-            if (WIDE) {  // a row's scale times its slabs'
+            if (LANE_IS_ROW) {  // a row's scale times its slabs'
               const float x = sc[quarter * 32u + lane];
               const float4 w = *reinterpret_cast<const float4*>(sc + ROWS + half * 4u);
               by[0] = pair(x * w.x, x * w.x), by[1 % FACTORS] = pair(x * w.y, x * w.y);
@@ -603,7 +661,10 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
               } else {
                 before_sync();
                 __syncwarp();
-                if (lane == 0) bar_arrive(&S.sums_empty[buf.at]);
+                if (lane == 0) {
+                  bar_arrive(&S.sums_empty[buf.at]);
+                  if (FORM == PAIR) bar_arrive_at<FORM>(at_first<FORM>(&S.both_empty[buf.at]));
+                }
                 buf.next(), slot.next();
                 if (b + DEPTH < n_blocks) first_read();
               }
@@ -611,12 +672,12 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
               if (r < PER || b + r / PER < n_blocks) {
 #pragma unroll
                 for (uint32_t c = 0; c < CHUNK; c += 2)
-                  add_products(sum[(r % PER * CHUNK + c) / 2], d[r % 2][c], d[r % 2][c + 1], by[WIDE ? r : (r * CHUNK + c) / 2]);
+                  add_products(sum[(r % PER * CHUNK + c) / 2], d[r % 2][c], d[r % 2][c + 1], by[LANE_IS_ROW ? r : (r * CHUNK + c) / 2]);
               }
             }
           }
           const bool failed = S.gave_up != 0u;
-          if (WIDE) {
+          if (LANE_IS_ROW) {
             const uint32_t rows_here = r0 < A.rows ? min(32u, A.rows - r0) : 0u;
             uint32_t* const words = reinterpret_cast<uint32_t*>(own);
             // One slab's code for all four: sums move down a slab's places each time.  (Code that is run once a tile has to be fetched each
@@ -703,10 +764,28 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
       block_sync();
     }
   }
+  // Nothing is in flight when a block ends: every copy has landed (a stage that not all the copying threads came to fill is filled up
+  // first), every product is through, and nobody writes to a block's barriers any more.
   before_sync();
   __syncthreads();
+  if (FORM == PAIR) pair_sync();
   after_sync();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tmem), "n"(TMEM) : "memory");
+  if (warp == 0 && lane == 0 && rank == 0) {
+    uint32_t most = 0u;
+    for (uint32_t i = 0; i < 2u * BLOCKS; ++i) most = max(most, S.copied[i]);
+    for (uint32_t i = 0; i < 2u * BLOCKS; ++i)
+      for (uint32_t k = S.copied[i]; k < most; ++k) bar_arrive(&S.full[k % Shape::stages]);
+    for (uint32_t k = most - min(most, Shape::stages); k < most; ++k) bar_drain(&S.full[k % Shape::stages], k / Shape::stages & 1u);
+  }
+  if (warp == 1 && lane == 0) bar_drain(&S.through, 0u);
+  before_sync();
+  __syncthreads();
+  if (FORM == PAIR) pair_sync();
+  after_sync();
+  if (warp == 1) {
+    if (FORM == PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(S.tmem), "n"(TMEM) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(S.tmem), "n"(TMEM) : "memory");
+  }
 }
 
 using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
@@ -733,34 +812,44 @@ struct HeadOperands {
   size_t hidden_stride, weight_stride;
 };
 
-template <typename T, uint32_t ROWS, bool WIDE>
+template <typename T, uint32_t ROWS, HeadForm FORM>
 fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, cudaStream_t st) {
-  using Shape = HeadShape<ROWS, WIDE>;
+  using Shape = HeadShape<ROWS, FORM>;
+  constexpr uint32_t BLOCKS = FORM == PAIR ? 2 : 1;
   CUtensorMap wmap, wmap4, xmap;
   if (!encode_tiled() || !byte_map(&wmap, O.weight, A.K, A.V, O.weight_stride, SLAB) || !byte_map(&wmap4, O.weight, A.K, A.V, O.weight_stride, 4 * SLAB) ||
       !byte_map(&xmap, O.hidden, A.K, A.rows, O.hidden_stride, ROWS)) {
     set_last_error("the operands cannot be described to the copy engine");
     return FMT_ERR_CUDA;
   }
-  auto* k = head_kernel<T, ROWS, WIDE>;
+  auto* k = head_kernel<T, ROWS, FORM>;
   if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::smem)) return launch_result(e);
-  // Rows that need several tiles: a block takes all of them for its slabs (the weights come from L2 after the first), unless
-  // the slabs divide badly among the blocks; then the tiles of rows are dealt out, too.
-  const uint32_t slabs = (A.V + SLAB - 1) / SLAB, row_tiles = (A.rows + ROWS - 1) / ROWS;
+  // Rows that need several tiles: a party takes all of them for its slabs (the weights come from L2 after the first), unless
+  // the slabs divide badly among the parties; then the tiles of rows are dealt out, too.
+  const uint32_t slabs = (A.V + SLAB - 1) / SLAB, row_tiles = (A.rows + BLOCKS * ROWS - 1) / (BLOCKS * ROWS), most = std::max(1u, sms / BLOCKS);
   uint32_t split = 1, least = 0xFFFFFFFFu;
-  for (uint32_t y = 1; y <= row_tiles && y <= sms; ++y) {
-    const uint32_t x = std::min(sms / y, slabs), each = (slabs + x - 1) / x, turns = (row_tiles + y - 1) / y;
+  for (uint32_t y = 1; y <= row_tiles && y <= most; ++y) {
+    const uint32_t x = std::min(most / y, slabs), each = (slabs + x - 1) / x, turns = (row_tiles + y - 1) / y;
     if (each * turns < least) least = each * turns, split = y;
   }
-  return launch_result(launch_overlapped(k, dim3(std::min(sms / split, slabs), split), dim3(HEAD_THREADS), Shape::smem, st, wmap, wmap4, xmap, A));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(std::min(most / split, slabs) * BLOCKS, split), cfg.blockDim = dim3(HEAD_THREADS), cfg.dynamicSmemBytes = Shape::smem, cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 2, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+  cfg.attrs = at, cfg.numAttrs = FORM == PAIR ? 2 : 1;
+  return launch_result(cudaLaunchKernelEx(&cfg, k, wmap, wmap4, xmap, A));
 }
 
 template <typename T>
 fmt_status head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, cudaStream_t st) {
-  if (A.rows <= 16) return launch_head<T, 16, false>(O, A, sms, st);
-  if (A.rows <= 32) return launch_head<T, 32, false>(O, A, sms, st);
-  if (A.rows <= 64) return launch_head<T, 64, false>(O, A, sms, st);
-  return launch_head<T, WIDE_ROWS, true>(O, A, sms, st);
+  if (A.rows <= 16) return launch_head<T, 16, FEW>(O, A, sms, st);
+  if (A.rows <= 32) return launch_head<T, 32, FEW>(O, A, sms, st);
+  if (A.rows <= 64) return launch_head<T, 64, FEW>(O, A, sms, st);
+  if (A.rows <= WIDE_ROWS) return launch_head<T, WIDE_ROWS, WIDE>(O, A, sms, st);
+  return launch_head<T, WIDE_ROWS, PAIR>(O, A, sms, st);
 }
 
 }  // namespace
