@@ -166,15 +166,10 @@ __device__ __forceinline__ void bar_init(uint64_t* b, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(uint64_t* b) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory");
 }
-template <bool CLUSTER = false>  // (whether the other block of a pair arrives there, too)
 __device__ __forceinline__ bool bar_test(uint64_t* b, uint32_t parity) {
   uint32_t done;
-  if (CLUSTER)
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done) : "r"(smem_addr(b)), "r"(parity) : "memory");
-  else
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done) : "r"(smem_addr(b)), "r"(parity) : "memory");
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(done) : "r"(smem_addr(b)), "r"(parity) : "memory");
   return done != 0u;
 }
 // The same variable in the memory of the pair's first block (of a block by itself: its own).
@@ -203,11 +198,10 @@ __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Waits until the barrier's phase of this parity is over.  False: given up, here or by another warp of the block.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, HeadShared& S) {
-  if (bar_test<CLUSTER>(b, parity)) return true;
+  if (bar_test(b, parity)) return true;
   for (uint32_t i = 0; i < WAIT_POLLS && !S.gave_up; ++i)
-    if (bar_test<CLUSTER>(b, parity)) return true;
+    if (bar_test(b, parity)) return true;
   S.gave_up = 1u;
   return false;
 }
@@ -520,21 +514,21 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
             const uint32_t there = min(SLABS, n_live - g), columns = FORM == FEW ? ROWS : FORM == WIDE ? there * SLAB : (there + 1u) / 2u * 2u * SLAB;
             const uint32_t idesc = 1u << 4 | (columns >> 3) << 17 | (BLOCKS * 128u >> 4) << 24;
             for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
-              if (!bar_wait<FORM == PAIR>(FORM == PAIR ? &S.both_empty[buf.at] : &S.sums_empty[buf.at], buf.round ^ 1u, S) ||
-                  !bar_wait<FORM == PAIR>(&S.full[stage.at], stage.round, S)) {
+              const uint32_t at = tiles_at + stage.at * Shape::stage_bytes, d = S.tmem + buf.at * BUF;
+              const uint64_t w = tile_desc(at), x = tile_desc(at + Shape::slabs_here * SLAB_BYTES);
+              // the copies are early, mostly; the sums' place is what it waits for
+              if (!bar_wait(&S.full[stage.at], stage.round, S) || !bar_wait(FORM == PAIR ? &S.both_empty[buf.at] : &S.sums_empty[buf.at], buf.round ^ 1u, S)) {
                 failed = true;
                 break;
               }
               after_sync();
-              const uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
-              const uint64_t w = tile_desc(at), x = tile_desc(at + Shape::slabs_here * SLAB_BYTES);
 #pragma unroll
               for (uint32_t k = 0; k < DEPTH; ++k)
                 if (k == 0 || b + k < n_blocks) {
 #pragma unroll
                   for (uint32_t i = 0; i < 4; ++i) {
                     const uint32_t more = (k * Shape::block_bytes + 32u * i) >> 4;
-                    mma<FORM>(S.tmem + buf.at * BUF + k * Shape::columns, (LANE_IS_ROW ? x : w) + more, (LANE_IS_ROW ? w : x) + more, idesc, i != 0);
+                    mma<FORM>(d + k * Shape::columns, (LANE_IS_ROW ? x : w) + more, (LANE_IS_ROW ? w : x) + more, idesc, i != 0);
                   }
                 }
               mma_commit<FORM>(&S.empty[stage.at]);
@@ -662,8 +656,8 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
                 before_sync();
                 __syncwarp();
                 if (lane == 0) {
-                  bar_arrive(&S.sums_empty[buf.at]);
                   if (FORM == PAIR) bar_arrive_at<FORM>(at_first<FORM>(&S.both_empty[buf.at]));
+                  bar_arrive(&S.sums_empty[buf.at]);
                 }
                 buf.next(), slot.next();
                 if (b + DEPTH < n_blocks) first_read();
