@@ -129,8 +129,8 @@ struct HeadShape {
   static constexpr uint32_t slabs = FORM == FEW ? 4 : 8;                        // of a tile
   static constexpr uint32_t slabs_here = FORM == PAIR ? 4 : slabs;              // of them in this block's memory
   static constexpr uint32_t columns = FORM == FEW ? ROWS : slabs * SLAB;        // of tensor memory
-  static constexpr uint32_t depth = FORM == FEW ? 2 : 1;                        // blocks of columns that make a stage: each round of waits costs some 400 cycles
-  static constexpr uint32_t stages = FORM == PAIR ? 6 : FORM == WIDE ? 4 : ROWS == 64 ? 4 : 5;
+  static constexpr uint32_t depth = FORM != FEW ? 1 : ROWS == 16 ? 4 : 2;       // blocks of columns that make a stage: each round of waits costs some 400 cycles
+  static constexpr uint32_t stages = FORM == PAIR ? 6 : FORM == WIDE ? 4 : ROWS == 64 ? 4 : ROWS == 32 ? 5 : 3;
   static constexpr uint32_t bufs = FORM == FEW ? 4 : 2;                         // of tensor memory, depth x columns each
   static constexpr uint32_t block_bytes = slabs_here * SLAB_BYTES + ROWS * BLOCK;
   static constexpr uint32_t stage_bytes = depth * block_bytes;

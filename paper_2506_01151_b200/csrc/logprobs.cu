@@ -343,7 +343,10 @@ __device__ __forceinline__ uint64_t max_key(uint64_t a, uint64_t b) { return a >
 // the n_top groups whose own largest reaches it hold any: their units alone are read again (L2), and what reaches the bound is
 // listed and put in order.  A row of 128,256 logits is passed once, and a sixth of it twice for n_top = 20, whatever its order.
 
-constexpr uint32_t THREADS = 256, PER_SM = 4, WARPS = THREADS / 32, UNROLL = 2, BACK_UNROLL = 1;
+constexpr uint32_t THREADS = 256, WARPS = THREADS / 32, UNROLL = 2, BACK_UNROLL = 1;
+// Blocks to an SM: four have 64 registers a thread, which a masked pass outgrows (2,048 rows of 128,256 bf16, four and three: masked 124 and
+// 109 us, unmasked 98.5 and 101).
+constexpr uint32_t per_sm(bool masked) { return masked ? 3u : 4u; }
 constexpr uint32_t GROUPS = 128, GROUP = THREADS / GROUPS;
 constexpr uint32_t MAX_CLUSTER = 8;
 constexpr uint32_t SORT = THREADS;                // listed logits that are put in order by counting
@@ -519,7 +522,7 @@ __device__ __forceinline__ void find_top(const Row<T>& row, const Keep<T>& keep,
 }
 
 template <typename T, bool MASK, bool TOP>
-__global__ void __launch_bounds__(THREADS, PER_SM) logprobs_kernel(const Rows R, const Outputs O, const uint32_t cluster) {
+__global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const Rows R, const Outputs O, const uint32_t cluster) {
   __shared__ JoinShared J;
   __shared__ Keep<T> keep;  // (of masked rows)
   __shared__ __align__(16) uint8_t top_raw[TOP ? sizeof(TopShared) : 16];
@@ -663,7 +666,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) logprobs_kernel(const Rows R,
 // since the gradient may take the logits' place.
 
 template <typename T, bool MASK>
-__global__ void __launch_bounds__(THREADS, PER_SM) logprobs_backward_kernel(const Rows R, const Gradients D, const uint32_t cluster) {
+__global__ void __launch_bounds__(THREADS, 4) logprobs_backward_kernel(const Rows R, const Gradients D, const uint32_t cluster) {
   __shared__ int32_t tok[FMT_MAX_GIVEN_TOKENS];
   __shared__ float g[FMT_MAX_GIVEN_TOKENS];
   __shared__ Keep<T> keep;
@@ -752,9 +755,9 @@ __global__ void __launch_bounds__(THREADS, PER_SM) logprobs_backward_kernel(cons
 // spends several microseconds on them however short its part is, so of those there are two to an SM (rows of 50,001 with 5
 // alternatives, 48 of them: 8 blocks a row 14.3 us, 4 12.2, 2 12.1; 64 rows of 128,256 with 20: 18.4, 15.1, 17.0), unless it
 // is for the second block (256 rows of 128,256 with 20: one 34.8, two 32.1, four 38.7).
-uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width, bool top) {
+uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width, uint32_t resident, bool top) {
   uint32_t c = 1;
-  while (c < MAX_CLUSTER && rows * (c * 2u) <= (top && c > 1 ? 2u : PER_SM) * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
+  while (c < MAX_CLUSTER && rows * (c * 2u) <= (top && c > 1 ? 2u : resident) * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
   return c;
 }
 
@@ -802,7 +805,7 @@ extern "C" fmt_status fmt_token_logprobs(const void* logits_dev, fmt_dtype dtype
                                 top_ids_dev, top_logprobs_dev, status_dev}))
     return s;
   const Outputs O{top_ids_dev || top_logprobs_dev ? n_top : 0u, logprobs_dev, norm_dev, entropy_dev, top_ids_dev, top_logprobs_dev, status_dev};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, O.n_top != 0);
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, per_sm(mask_dev != nullptr), O.n_top != 0);
   void (*k)(Rows, Outputs, uint32_t);
   if (dtype == FMT_BF16)
     k = mask_dev ? O.n_top ? logprobs_kernel<uint16_t, true, true> : logprobs_kernel<uint16_t, true, false>
@@ -832,7 +835,7 @@ extern "C" fmt_status fmt_token_logprobs_backward(const void* logits_dev, fmt_dt
                                 grad_entropy_dev, grad_logits_dev}))
     return s;
   const Gradients D{norm_dev, entropy_dev, grad_logprobs_dev, grad_entropy_dev, grad_logits_dev, grad_stride_elems};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, false);
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, 4, false);
   auto* k = dtype == FMT_BF16 ? mask_dev ? logprobs_backward_kernel<uint16_t, true> : logprobs_backward_kernel<uint16_t, false>
                               : mask_dev ? logprobs_backward_kernel<float, true> : logprobs_backward_kernel<float, false>;
   return launch_result(launch_clusters(k, rows, cluster, (cudaStream_t)stream, R, D, cluster));
