@@ -751,13 +751,13 @@ __global__ void __launch_bounds__(THREADS, 4) logprobs_backward_kernel(const Row
   });
 }
 
-// Blocks to a row: as many as run at a time, while each has a unit for every thread at least.  A block that looks for alternatives
-// spends several microseconds on them however short its part is, so of those there are two to an SM (rows of 50,001 with 5
-// alternatives, 48 of them: 8 blocks a row 14.3 us, 4 12.2, 2 12.1; 64 rows of 128,256 with 20: 18.4, 15.1, 17.0), unless it
-// is for the second block (256 rows of 128,256 with 20: one 34.8, two 32.1, four 38.7).
+// Blocks to a row: as many as run at a time (`resident` to an SM), while each has a unit for every thread at least.  A block that
+// looks for alternatives spends several microseconds on them however short its part is, so of those there are two to an SM (rows of
+// 50,001 with 5 alternatives, 48 of them: 8 blocks a row 14.3 us, 4 12.2, 2 12.1; 64 rows of 128,256 with 20: 18.4, 15.1, 17.0).  The
+// second block is worth it even so (256 masked rows of 128,256 with 20 alternatives: one 39.2, two 30.9, four 38.7; without: 31, 20).
 uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width, uint32_t resident, bool top) {
   uint32_t c = 1;
-  while (c < MAX_CLUSTER && rows * (c * 2u) <= (top && c > 1 ? 2u : resident) * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
+  while (c < MAX_CLUSTER && rows * (c * 2u) <= (c == 1 ? 4u : top ? 2u : resident) * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
   return c;
 }
 
