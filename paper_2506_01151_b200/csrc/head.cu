@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
         uint32_t any = 0u;
         if (no < n_slabs) {
 #pragma unroll 8
-          for (uint32_t r = 0; r < A.rows; ++r) any |= __ldg(A.mask + (size_t)r * A.mask_stride + no);
+          for (uint32_t r = 0; r < A.rows; ++r) any |= A.mask[(size_t)r * A.mask_stride + no];
         }
         const uint32_t word = __ballot_sync(0xFFFFFFFFu, any != 0u);
         if (lane == 0) S.bits[i] = word;
@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
         for (uint32_t r0 = 0; r0 < A.rows && !any; r0 += 256) {
 #pragma unroll
           for (uint32_t u = 0; u < 8; ++u)
-            if (r0 + u * 32u + lane < A.rows) any |= __ldg(m + (size_t)(r0 + u * 32u + lane) * A.mask_stride);
+            if (r0 + u * 32u + lane < A.rows) any |= m[(size_t)(r0 + u * 32u + lane) * A.mask_stride];
           any = __any_sync(0xFFFFFFFFu, any != 0u);
         }
         if (lane == 0 && any) atomicOr(&S.bits[i / 32], 1u << (i % 32));
@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
           for (uint32_t i = 0; i < WORDS; ++i) {
             word[i] = 0xFFFFFFFFu;
             if (A.mask && (LANE_IS_ROW ? i < mine : mine && lane < COLS) && r0 + lane < A.rows)
-              word[i] = __ldg(A.mask + (size_t)(r0 + lane) * A.mask_stride + S.live[g + (LANE_IS_ROW ? half * 4u + i : quarter)]);
+              word[i] = A.mask[(size_t)(r0 + lane) * A.mask_stride + S.live[g + (LANE_IS_ROW ? half * 4u + i : quarter)]];
           }
           uint64_t sum[COLS / 2];
 #pragma unroll

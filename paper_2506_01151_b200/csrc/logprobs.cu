@@ -205,11 +205,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 }
 
 // A unit's values in pairs, nothing below LOW (-inf becomes LOW; a NaN stays).  LOW lies so far below a row's largest logit that
-// its probability is 0, and is finite, so that 0 times what is made of it is 0.  This holds for rows whose largest logit is above
-// LOW / 10 and whose temperature is between 2e-6 and 1e8 (`ordinary`): 0.9 x 2^40 x 1e-8 is 9,900 powers of two.  In others
-// every value is looked at.
+// its probability is 0, and is finite, so that 0 times what is made of it is 0.  This holds for rows whose largest logit is between
+// LOW / 10 and -LOW / 10 and whose temperature is between 2e-6 and 1e8 (`ordinary`): 0.9 x 2^40 x 1e-8 is 9,900 powers of two, and
+// 1.1 x 2^40 x 1e6 a number.  In others every value is looked at.
 constexpr float LOW = -0x1p40f;
-__device__ __forceinline__ bool ordinary(float largest, float c) { return largest > LOW * 0.1f && c > 1e-8f && c < 1e6f; }
+__device__ __forceinline__ bool ordinary(float largest, float c) { return fabsf(largest) < LOW * -0.1f && c > 1e-8f && c < 1e6f; }
 __device__ __forceinline__ uint64_t pair_of(const Unit& x, uint32_t i, uint16_t) {
   uint32_t w;
   asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w) : "r"(x.v[i]), "r"(0xD380D380u));
@@ -223,8 +223,9 @@ __device__ __forceinline__ uint64_t pair_of(const Unit& x, uint32_t i, float) {
 }
 
 // A thread's units from, from + step, ..., N at a time: the next N are on their way, and the bits of those after them, while
-// work(first, units) is at some.  What the mask forbids, and what is behind the row's last unit, is -inf.
-template <typename T, bool MASK, bool ALIGNED, uint32_t N, class F>
+// work(first, units) is at some.  What the mask forbids, and what is behind the row's last unit, is -inf.  SKIP: without work where
+// nothing is allowed.
+template <typename T, bool MASK, bool ALIGNED, bool SKIP, uint32_t N, class F>
 __device__ __forceinline__ void row_turns_of(const Row<T>& row, uint32_t from, uint32_t step, const Keep<T>& keep, F work) {
   const uint32_t n = row.units, stride = N * step;
   auto ask_bits = [&](uint32_t i, uint32_t (&to)[N]) {
@@ -239,15 +240,20 @@ __device__ __forceinline__ void row_turns_of(const Row<T>& row, uint32_t from, u
   uint32_t ba[N], bb[N];
   auto turn = [&](uint32_t i, Unit (&x)[N], uint32_t (&bits)[N], Unit (&next)[N], const uint32_t (&ahead)[N]) {
     ask(i + stride, ahead, next);
+    uint32_t any = 1u;
     if (MASK) {
+      if (SKIP) any = 0u;
 #pragma unroll
-      for (uint32_t u = 0; u < N; ++u) forbid(x[u], keep, bits[u]);
+      for (uint32_t u = 0; u < N; ++u) {
+        forbid(x[u], keep, bits[u]);
+        if (SKIP) any |= bits[u];
+      }
     } else if (i + (N - 1u) * step >= n) {
 #pragma unroll
       for (uint32_t u = 1; u < N; ++u) forbid<T>(x[u], bits[u]);
     }
     ask_bits(i + 2u * stride, bits);
-    work(i, x);
+    if (any) work(i, x);
   };
   ask_bits(from, ba);
   ask(from, ba, xa);
@@ -258,10 +264,10 @@ __device__ __forceinline__ void row_turns_of(const Row<T>& row, uint32_t from, u
   }
 }
 
-template <typename T, bool MASK, uint32_t N, class F>
+template <typename T, bool MASK, bool SKIP, uint32_t N, class F>
 __device__ __forceinline__ void row_turns(const Row<T>& row, uint32_t from, uint32_t step, const Keep<T>& keep, F work) {
-  if (MASK && row.head == 0) row_turns_of<T, MASK, true, N>(row, from, step, keep, work);
-  else row_turns_of<T, MASK, false, N>(row, from, step, keep, work);
+  if (MASK && row.head == 0) row_turns_of<T, MASK, true, SKIP, N>(row, from, step, keep, work);
+  else row_turns_of<T, MASK, false, SKIP, N>(row, from, step, keep, work);
 }
 
 // ------------------------------------------------------------------------------------------------ sums of a row
@@ -555,7 +561,7 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
   }
 
   const uint32_t from = rank * THREADS + tid, step = cluster * THREADS;
-  row_turns<T, MASK, UNROLL>(row, from, step, keep, [&](uint32_t i, const Unit (&x)[UNROLL]) {
+  row_turns<T, MASK, true, UNROLL>(row, from, step, keep, [&](uint32_t i, const Unit (&x)[UNROLL]) {
     const float most = largest(x, T());
     if (most > a.m) {
       if (TOP) where = i;
@@ -707,7 +713,7 @@ __global__ void __launch_bounds__(THREADS, 4) logprobs_backward_kernel(const Row
   const bool is_ordinary = ordinary(most, c);
   const uint64_t most2 = two(-most, -most), c2 = two(0.5f * c, 0.5f * c), log2s2 = two(-0.5f * log2s, -0.5f * log2s), A2 = two(A, A), B2 = two(2.0f * B, 2.0f * B);
   const uint32_t step = cluster * THREADS;
-  row_turns<T, MASK, BACK_UNROLL>(row, rank * THREADS + tid, step, keep, [&](uint32_t first, const Unit (&x)[BACK_UNROLL]) {
+  row_turns<T, MASK, false, BACK_UNROLL>(row, rank * THREADS + tid, step, keep, [&](uint32_t first, const Unit (&x)[BACK_UNROLL]) {
 #pragma unroll
     for (uint32_t u = 0; u < BACK_UNROLL; ++u) {
       const uint32_t i = first + u * step, v = row.first(i);

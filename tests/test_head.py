@@ -172,6 +172,42 @@ def test_odd_sizes(V, K):
 
 
 @gpu
+@pytest.mark.parametrize("n", [16, 40, 70, 200])
+@pytest.mark.parametrize("V", [1, 33, 100, 200, 4737])
+@pytest.mark.parametrize("K", [1, 129, 700])
+def test_odd_sizes_of_every_form(K, V, n):
+    h = Head(n, V, K, "mixed", dtype="bf16" if K % 2 else "fp32", seed=V + K, pad=K % 3, offset=n % 3, row_pad=V % 5, mask_pad=K % 2)
+    h.call()
+    h.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("offset,row_pad", [(0, 0), (2, 0), (1, 1), (16, 16)])
+@pytest.mark.parametrize("n", [20, 100, 300])
+def test_rows_begin_at_any_address(n, offset, row_pad, dtype):
+    h = Head(n, 3200, 256, "mixed", dtype, seed=n, offset=offset, row_pad=row_pad)
+    h.call()
+    h.check()
+
+
+@gpu
+@pytest.mark.parametrize("n", [8, 300])
+def test_sparse_masks_of_large_vocabularies(n):
+    """From one word in a hundred to every other word in use: the lists of slabs, whole and piecewise."""
+    torch = torch_()
+    for share in (0.01, 0.1, 0.5, 0.97):
+        h = Head(n, 40000, 300, "all", "bf16", seed=int(share * 100))
+        g = torch.Generator(device=DEV)
+        g.manual_seed(3)
+        words = torch.rand(h.words, generator=g, device=DEV) < share
+        h.allow = words.repeat_interleave(32)[None, :40000].expand(n, -1).clone()
+        h.mask = torch.where(words, -1, 0).to(torch.int32)[None].repeat(n, 1).contiguous()
+        h.call()
+        h.check()
+
+
+@gpu
 @pytest.mark.parametrize("mask", ["all", "few", "empty"])
 @pytest.mark.parametrize("n,V,K,dtype", [(1, 32000, 4096, "bf16"), (8, 128256, 1024, "bf16"), (37, 50001, 2880, "fp32"), (300, 20011, 512, "bf16"), (256, 128256, 256, "bf16"), (1500, 6000, 1030, "bf16")])
 def test_large(n, V, K, dtype, mask):

@@ -257,6 +257,34 @@ def test_alternatives_wherever_they_lie(order, n_top):
 
 
 @gpu
+@pytest.mark.parametrize("n", [2, 600])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("every,of", [(64, 256), (512, 2048), (1, 4), (3, 97)])
+def test_alternatives_crowded_in_some_places(every, of, dtype, n):
+    """Thousands of logits that are larger than all others, side by side in stretches of 32 bytes: more than any list holds."""
+    torch = torch_()
+    V = 40000
+    i = Inputs(n, V, dtype, "mixed" if every == 1 else "none", heat=False, n_tokens=1, seed=every)
+    unit = torch.arange(V, device=DEV) // (16 if dtype == "bf16" else 8)
+    i.logits += torch.where(unit % of < every, 40.0, 0.0).to(i.type)
+    for n_top in (20, 32):
+        check_forward(i, i.forward(n_top), n_top)
+
+
+@gpu
+@pytest.mark.parametrize("temperature", [1e-30, 1e-9, 1.9e-6, 1e-3, 1e4, 1.5e8, 1e30])
+@pytest.mark.parametrize("scale,shift", [(1.0, 0.0), (1.0, -2e11), (1e12, 0.0), (1e20, -1e21), (1e-20, 0.0), (3e37, 0.0)])
+def test_extreme_temperatures_and_logits(scale, shift, temperature):
+    i = Inputs(3, 5003, "fp32", "mixed", seed=7, scale=scale)
+    i.logits += shift
+    i.temperature[:] = temperature
+    out = i.forward()
+    want = check_forward(i, out)
+    if scale * 10 / temperature < 1e30 and 1e-20 < temperature:  # (where the gradient, or the exponents' errors, are no numbers of fp32)
+        check_backward(i, i.backward(out), want)
+
+
+@gpu
 @pytest.mark.parametrize("n_tokens", [0, 1, 32])
 @pytest.mark.parametrize("with_g,with_h", [(True, False), (False, True), (False, False)])
 def test_gradients_that_are_not_given(n_tokens, with_g, with_h):
