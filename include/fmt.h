@@ -4,7 +4,8 @@
  * The library implements the per-step token mask of "Earley-Driven Dynamic Pruning for
  * Efficient Structured Decoding" (ZapFormat / Formatron): every vocabulary token's bytes are
  * fed through each sequence's pruned Earley chart and the token is valid iff the chart stays
- * non-empty (Sections 3.2, 3.3, 4.1, 4.2 of the paper).
+ * non-empty (Sections 3.2, 3.3, 4.1, 4.2 of the paper).  Around the mask stand the output head,
+ * which makes the logits (fmt_head_logits), and what is read off them (fmt_token_logprobs).
  *
  * Conventions
  *  - Every function returns fmt_status (FMT_OK = 0).  No exception crosses this boundary.
