@@ -811,7 +811,11 @@ fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, int dev, uint32
   using Shape = HeadShape<ROWS, FORM>;
   constexpr uint32_t BLOCKS = FORM == PAIR ? 2 : 1;
   CUtensorMap wmap, wmap4, xmap;
-  if (!encode_tiled() || !byte_map(&wmap, O.weight, A.K, A.V, O.weight_stride, SLAB) || !byte_map(&wmap4, O.weight, A.K, A.V, O.weight_stride, 4 * SLAB) ||
+  if (!encode_tiled()) {
+    set_last_error("the driver has no cuTensorMapEncodeTiled");
+    return FMT_ERR_CUDA;
+  }
+  if (!byte_map(&wmap, O.weight, A.K, A.V, O.weight_stride, SLAB) || !byte_map(&wmap4, O.weight, A.K, A.V, O.weight_stride, 4 * SLAB) ||
       !byte_map(&xmap, O.hidden, A.K, A.rows, O.hidden_stride, ROWS)) {
     return refuse("the operands cannot be described to the copy engine (a stride of 2^40 bytes or more?)");
   }

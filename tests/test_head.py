@@ -192,6 +192,16 @@ def test_rows_begin_at_any_address(n, offset, row_pad, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("n,V,mask", [(3, 2600000, "few"), (3, 2600000, "none"), (130, 1300000, "few"), (130, 1300000, "mixed")])
+def test_more_slabs_than_a_list_holds(n, V, mask):
+    h = Head(n, V, 16, mask, "bf16", seed=n)
+    h.call()
+    h.check()
+    del h
+    torch_().cuda.empty_cache()
+
+
+@gpu
 @pytest.mark.parametrize("n", [8, 300])
 def test_sparse_masks_of_large_vocabularies(n):
     """From one word in a hundred to every other word in use: the lists of slabs, whole and piecewise."""
@@ -360,6 +370,9 @@ def test_memory_that_the_device_cannot_reach_is_refused():
         setattr(h, name, kept.cpu())
         refused(h.call)
         setattr(h, name, kept)
+    h.ws = 1 << 40  # more than the copy engine can step
+    refused(h.call)
+    h.ws = 128
     x, q, s = torch.zeros((2, 64), device=DEV), torch.zeros((2, 64), dtype=torch.uint8, device=DEV), torch.zeros((1, 2), device=DEV)
     refused(fmt.quantize_blocks, x.cpu(), fmt.FP32, 2, 64, 1, q, s)
     refused(fmt.quantize_blocks, x, fmt.FP32, 2, 64, 1, q.cpu(), s)
