@@ -130,9 +130,10 @@ def _ptr(x) -> Optional[int]:
     """Device pointer of a torch tensor, or a raw integer / None."""
     if x is None:
         return None
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr()
-    return int(x)
+    except AttributeError:
+        return int(x)
 
 
 _TABLE_DTYPES = {0: np.uint32, 1: np.uint8, 2: np.uint32, 3: np.uint32, 4: np.uint32, 5: np.uint32, 6: np.uint8,

@@ -316,6 +316,13 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&b);
 }
 
+// A pair of bf16, -inf where the bytes of `bits` that `which` names do not have their highest bits.
+__device__ __forceinline__ uint32_t keep_pair(uint32_t x, uint32_t bits, uint32_t which) {
+  uint32_t k;
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(k) : "r"(bits), "r"(which));  // (selectors 8 and up repeat a byte's highest bit)
+  return (x & k) | (0xFF80FF80u & ~k);
+}
+
 template <typename T, uint32_t ROWS, HeadForm FORM>
 __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap wmap4,
                                                                const __grid_constant__ CUtensorMap xmap, const HeadArgs A) {
@@ -619,16 +626,16 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
           uint64_t sum[COLS / 2];
 #pragma unroll
           for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = 0;
-          // One piece is read while the one before is added, the first of the next stage (if it is there) with the last of this one.
+          // Two pieces are on their way at a time; the first two of the next stage (if it is there) while the last two of this one are added.
           float d[2][CHUNK];
           const uint32_t lanes = S.tmem + (quarter * 32u << 16) + half * COLS;
           auto read = [&](uint32_t r) { tmem_read<CHUNK>(lanes + buf.at * BUF + r * CHUNK / COLS * Shape::columns + r * CHUNK % COLS, d[r % 2]); };
-          auto first_read = [&] {
+          auto stage_ready = [&] {
             bar_wait_on(&S.sums_full[buf.at], buf.round, S);
             after_sync();
-            read(0);
           };
-          first_read();
+          stage_ready();
+          read(0), read(1);
           for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
             uint64_t by[FACTORS];  // the products of two scales
             const float* sc = scales + slot.at * Shape::slot_floats;
@@ -648,12 +655,19 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
                 }
               }
             }
+            constexpr uint32_t PER = COLS / CHUNK;  // reads of a block of columns
+            auto add = [&](uint32_t r) {
+              if (r < PER || b + r / PER < n_blocks) {
 #pragma unroll
-            for (uint32_t r = 0; r < READS; ++r) {
+                for (uint32_t c = 0; c < CHUNK; c += 2)
+                  add_products(sum[(r % PER * CHUNK + c) / 2], d[r % 2][c], d[r % 2][c + 1], by[LANE_IS_ROW ? r : (r * CHUNK + c) / 2]);
+              }
+            };
+            const bool more = b + DEPTH < n_blocks;
+#pragma unroll
+            for (uint32_t r = 0; r < READS; r += 2) {
               tmem_read_done();
-              if (r + 1 < READS) {
-                read(r + 1);
-              } else {
+              if (r + 2 == READS) {
                 before_sync();
                 __syncwarp();
                 if (lane == 0) {
@@ -661,18 +675,54 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
                   bar_arrive(&S.sums_empty[buf.at]);
                 }
                 buf.next(), slot.next();
-                if (b + DEPTH < n_blocks) first_read();
               }
-              constexpr uint32_t PER = COLS / CHUNK;  // reads of a block of columns
-              if (r < PER || b + r / PER < n_blocks) {
-#pragma unroll
-                for (uint32_t c = 0; c < CHUNK; c += 2)
-                  add_products(sum[(r % PER * CHUNK + c) / 2], d[r % 2][c], d[r % 2][c + 1], by[LANE_IS_ROW ? r : (r * CHUNK + c) / 2]);
-              }
+              add(r);
+              if (r + 2 < READS) read(r + 2);
+              else if (more) stage_ready(), read(0);
+              add(r + 1);
+              if (r + 2 < READS) read(r + 3);
+              else if (more) read(1);
             }
           }
-          const bool failed = S.gave_up != 0u;
-          if (LANE_IS_ROW) {
+          if (S.gave_up) {
+#pragma unroll
+            for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = pair(nan, nan);
+          }
+          if (LANE_IS_ROW && by_units && S.live[g + min(count, SLABS) - 1u] * SLAB + SLAB <= A.V) {
+            // a lane holds 32 tokens of a row for each slab, which are two (bf16) or four units of 32 bytes
+            if (r0 + lane < A.rows) {
+#pragma unroll
+              for (uint32_t i = 0; i < 4; ++i) {
+                if (i >= mine) break;
+                uint32_t* const to = reinterpret_cast<uint32_t*>(logits + (size_t)(r0 + lane) * A.row_stride + S.live[g + half * 4u + i] * SLAB);
+                const uint32_t allowed = word[i % WORDS];
+                uint32_t y[sizeof(T) * SLAB / 4];
+#pragma unroll
+                for (uint32_t c = 0; c < SLAB; c += 2) {
+                  const uint64_t two = sum[(i * SLAB + c) / 2 % (COLS / 2)];
+                  if (sizeof(T) == 2) y[c / 2] = two_bf16(part(two, 0), part(two, 1));
+                  else y[c % (sizeof(y) / 4)] = (uint32_t)two, y[(c + 1) % (sizeof(y) / 4)] = (uint32_t)(two >> 32);
+                }
+                if (allowed != 0xFFFFFFFFu) {
+                  if (sizeof(T) == 2) {
+#pragma unroll
+                    for (uint32_t c = 0; c < SLAB; c += 4) {
+                      const uint32_t bits = ((allowed >> c & 15u) * 0x00204081u & 0x01010101u) << 7;  // each bit the highest of a byte
+                      y[c / 2] = keep_pair(y[c / 2], bits, 0x9988u), y[c / 2 + 1] = keep_pair(y[c / 2 + 1], bits, 0xBBAAu);
+                    }
+                  } else {
+#pragma unroll
+                    for (uint32_t c = 0; c < SLAB; ++c) y[c % (sizeof(y) / 4)] = (allowed >> c) & 1u ? y[c % (sizeof(y) / 4)] : 0xFF800000u;
+                  }
+                }
+#pragma unroll
+                for (uint32_t q = 0; q < sizeof(y) / 4; q += 8)
+                  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + q), "r"(y[q]), "r"(y[q + 1]), "r"(y[q + 2]), "r"(y[q + 3]),
+                               "r"(y[q + 4]), "r"(y[q + 5]), "r"(y[q + 6]), "r"(y[q + 7])
+                               : "memory");
+              }
+            }
+          } else if (LANE_IS_ROW) {
             const uint32_t rows_here = r0 < A.rows ? min(32u, A.rows - r0) : 0u;
             uint32_t* const words = reinterpret_cast<uint32_t*>(own);
             // One slab's code for all four, which has to be fetched for every tile: sums move down a slab's places each time.
@@ -688,26 +738,10 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
               for (uint32_t c = SLAB / 2; c < COLS / 2; ++c) sum[(c - SLAB / 2) % (COLS / 2)] = sum[c];
 #pragma unroll
               for (uint32_t k = 1; k < WORDS; ++k) word[k - 1] = word[k];
-              auto masked = [&](uint32_t c) {
-                const float y = failed ? nan : part(now[c / 2], c % 2);
-                return (allowed >> c) & 1u ? y : minus_inf;
-              };
+              auto masked = [&](uint32_t c) { return (allowed >> c) & 1u ? part(now[c / 2], c % 2) : minus_inf; };
               auto packed = [&](uint32_t c) {  // word c of the slab's row
                 return sizeof(T) == 4 ? __float_as_uint(masked(c % SLAB)) : two_bf16(masked(2 * c % SLAB), masked((2 * c + 1) % SLAB));
               };
-              if (by_units && v0 + SLAB <= A.V) {
-                // a lane holds 32 tokens of a row, which are two (bf16) or four units of 32 bytes
-                if (lane < rows_here) {
-                  T* const to = logits + (size_t)(r0 + lane) * A.row_stride + v0;
-#pragma unroll
-                  for (uint32_t q = 0; q < sizeof(T) * SLAB / 4; q += 8)
-                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(reinterpret_cast<uint32_t*>(to) + q), "r"(packed(q)),
-                                 "r"(packed(q + 1)), "r"(packed(q + 2)), "r"(packed(q + 3)), "r"(packed(q + 4)), "r"(packed(q + 5)), "r"(packed(q + 6)),
-                                 "r"(packed(q + 7))
-                                 : "memory");
-                }
-                continue;
-              }
               // rows that begin elsewhere: turned round in shared memory, 16 words of a row at a time, so that a warp writes them side by side
               constexpr uint32_t TOKENS = TURN * 4 / sizeof(T);
 #pragma unroll
@@ -747,7 +781,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
 #pragma unroll
               for (uint32_t c = 0; c < 8; ++c, to += A.row_stride) {
                 const uint32_t m = __shfl_sync(0xFFFFFFFFu, word[0], c0 + c);
-                const float y = !((m >> lane) & 1u) ? minus_inf : failed ? nan : part(sum[c / 2], c % 2);
+                const float y = (m >> lane) & 1u ? part(sum[c / 2], c % 2) : minus_inf;
                 if (r0 + c0 + c < A.rows && v < A.V) put(to, y);
               }
 #pragma unroll
