@@ -437,7 +437,7 @@ fmt_status fmt_quantize_blocks(const void* x_dev, fmt_dtype dtype, uint32_t rows
  *   weight_dev   [V][K] e4m3 bytes and weight_scales_dev, as it writes them with block_rows = 128
  *   hidden_stride, weight_stride  bytes from row to row, at least K, multiples of 16; both arrays 16-byte aligned
  *   mask_dev     [rows][mask_stride_words] packed masks (fmt_fill_mask), or NULL: every token is allowed
- * K at most 2^20, rows and V at most 2^24.  Every wait inside the kernel is a poll with an iteration limit; should one run out,
+ * K and V at most 2^20, rows at most 2^24.  Every wait inside the kernel is a poll with an iteration limit; should one run out,
  * the logits that are not computed become NaN.
  */
 fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_stride, const float* hidden_scales_dev, size_t hidden_scale_stride,

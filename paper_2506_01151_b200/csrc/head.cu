@@ -112,7 +112,8 @@ __global__ void __launch_bounds__(QUANTIZE_WARPS * 32) quantize_kernel(const T* 
 
 constexpr uint32_t SLAB = 32;
 constexpr uint32_t HEAD_THREADS = 384, ADD_WARPS = 8;
-constexpr uint32_t LIST = 512;        // slabs of a block that are looked at in one go
+constexpr uint32_t LIST = 512;        // slabs of a block, at most
+constexpr uint32_t MOST_TOKENS = 1u << 20;
 constexpr uint32_t ALL_SLABS = 8192;  // of a vocabulary whose masks every block looks at as a whole
 constexpr uint32_t ALL_WORDS = 32768; // of the masks then
 constexpr uint32_t SCALE_SLOTS = 8;
@@ -271,7 +272,6 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
   else
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
-__device__ __forceinline__ void block_sync() { asm volatile("bar.sync 1, %0;" ::"n"(HEAD_THREADS) : "memory"); }  // from wherever a warp is
 __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
@@ -376,65 +376,61 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
   // Small masks are looked at as a whole by every block, and what is left of the vocabulary is dealt out anew: where a grammar leaves
   // few tokens, a block's own slabs have five or six of them, or none (8 rows of 32,000 x 4,096: 19.2 us, so 13.4).
   const bool whole = A.mask && n_slabs <= ALL_SLABS && (uint64_t)n_slabs * A.rows <= ALL_WORDS && n_slabs > parties && n_mine < LIST;
-  // The block's slabs from the first-th on that some row may use, and the others.  All threads.
-  auto list_slabs = [&](uint32_t first) {
-    if (whole) {
-      // lanes are slabs: their words lie side by side
-      for (uint32_t i = warp; i < (n_slabs + 31u) / 32u; i += HEAD_THREADS / 32) {
-        const uint32_t no = i * 32u + lane;
-        uint32_t any = 0u;
-        if (no < n_slabs) {
+  // The block's slabs that some row may use, and the others.
+  if (whole) {
+    // lanes are slabs: their words lie side by side
+    for (uint32_t i = warp; i < (n_slabs + 31u) / 32u; i += HEAD_THREADS / 32) {
+      const uint32_t no = i * 32u + lane;
+      uint32_t any = 0u;
+      if (no < n_slabs) {
 #pragma unroll 8
-          for (uint32_t r = 0; r < A.rows; ++r) any |= A.mask[(size_t)r * A.mask_stride + no];
-        }
-        const uint32_t word = __ballot_sync(0xFFFFFFFFu, any != 0u);
-        if (lane == 0) S.bits[i] = word;
+        for (uint32_t r = 0; r < A.rows; ++r) any |= A.mask[(size_t)r * A.mask_stride + no];
       }
-      block_sync();
-      if (warp == 0) {  // the slabs that some row may use are dealt out among the blocks as all are otherwise
-        uint32_t seen = 0;
-        for (uint32_t i = 0; i < (n_slabs + 31u) / 32u; i += 32) {
-          uint32_t upto = i + lane < (n_slabs + 31u) / 32u ? __popc(S.bits[i + lane]) : 0u;
-#pragma unroll
-          for (uint32_t o = 1; o < 32u; o <<= 1) {
-            const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-            if (lane >= o) upto += x;
-          }
-          upto += seen;
-          if (i + lane < ALL_SLABS / 32) S.upto[i + lane] = upto;  // how many there are up to the end of this word
-          seen = __shfl_sync(0xFFFFFFFFu, upto, 31);
-        }
-        __syncwarp();
-        const uint32_t by_four = seen / (4u * parties), n_live = share(seen, by_four);
-        for (uint32_t k = lane; k < n_live; k += 32) {
-          const uint32_t no = place(k, by_four);  // among those
-          uint32_t lo = 0, hi = (n_slabs + 31u) / 32u - 1u;
-          while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (S.upto[mid] > no) hi = mid;
-            else lo = mid + 1;
-          }
-          S.live[k] = lo * 32u + __fns(S.bits[lo], 0, (int)(no - (lo ? S.upto[lo - 1] : 0u)) + 1);
-        }
-        uint32_t n_dead = 0;
-        for (uint32_t k = lane; k < (n_mine + 31u) / 32u * 32u; k += 32) {
-          const uint32_t no = k < n_mine ? slab_no(k) : 0u;
-          const bool gone = k < n_mine && !((S.bits[no / 32u] >> (no % 32u)) & 1u);
-          const uint32_t all = __ballot_sync(0xFFFFFFFFu, gone);
-          if (gone) S.dead[n_dead + __popc(all & ((1u << lane) - 1u))] = no;
-          n_dead += __popc(all);
-        }
-        if (lane == 0) S.n_live = n_live, S.n_dead = n_dead;
-      }
-      block_sync();
-      return;
+      const uint32_t word = __ballot_sync(0xFFFFFFFFu, any != 0u);
+      if (lane == 0) S.bits[i] = word;
     }
-    const uint32_t here = min(LIST, n_mine - first);
+    __syncthreads();
+    if (warp == 0) {  // the slabs that some row may use are dealt out among the blocks as all are otherwise
+      uint32_t seen = 0;
+      for (uint32_t i = 0; i < (n_slabs + 31u) / 32u; i += 32) {
+        uint32_t upto = i + lane < (n_slabs + 31u) / 32u ? __popc(S.bits[i + lane]) : 0u;
+#pragma unroll
+        for (uint32_t o = 1; o < 32u; o <<= 1) {
+          const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+          if (lane >= o) upto += x;
+        }
+        upto += seen;
+        if (i + lane < ALL_SLABS / 32) S.upto[i + lane] = upto;  // how many there are up to the end of this word
+        seen = __shfl_sync(0xFFFFFFFFu, upto, 31);
+      }
+      __syncwarp();
+      const uint32_t by_four = seen / (4u * parties), n_live = share(seen, by_four);
+      for (uint32_t k = lane; k < n_live; k += 32) {
+        const uint32_t no = place(k, by_four);  // among those
+        uint32_t lo = 0, hi = (n_slabs + 31u) / 32u - 1u;
+        while (lo < hi) {
+          const uint32_t mid = (lo + hi) / 2;
+          if (S.upto[mid] > no) hi = mid;
+          else lo = mid + 1;
+        }
+        S.live[k] = lo * 32u + __fns(S.bits[lo], 0, (int)(no - (lo ? S.upto[lo - 1] : 0u)) + 1);
+      }
+      uint32_t n_dead = 0;
+      for (uint32_t k = lane; k < (n_mine + 31u) / 32u * 32u; k += 32) {
+        const uint32_t no = k < n_mine ? slab_no(k) : 0u;
+        const bool gone = k < n_mine && !((S.bits[no / 32u] >> (no % 32u)) & 1u);
+        const uint32_t all = __ballot_sync(0xFFFFFFFFu, gone);
+        if (gone) S.dead[n_dead + __popc(all & ((1u << lane) - 1u))] = no;
+        n_dead += __popc(all);
+      }
+      if (lane == 0) S.n_live = n_live, S.n_dead = n_dead;
+    }
+  } else {
     if (tid < LIST / 32) S.bits[tid] = A.mask ? 0u : 0xFFFFFFFFu;
-    block_sync();
+    __syncthreads();
     if (A.mask)
-      for (uint32_t i = warp; i < here; i += HEAD_THREADS / 32) {
-        const uint32_t* m = A.mask + slab_no(first + i);
+      for (uint32_t i = warp; i < n_mine; i += HEAD_THREADS / 32) {
+        const uint32_t* m = A.mask + slab_no(i);
         uint32_t any = 0u;
         for (uint32_t r0 = 0; r0 < A.rows && !any; r0 += 256) {
 #pragma unroll
@@ -444,146 +440,142 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
         }
         if (lane == 0 && any) atomicOr(&S.bits[i / 32], 1u << (i % 32));
       }
-    block_sync();
+    __syncthreads();
     if (warp == 0) {
       uint32_t n_live = 0, n_dead = 0;
-      for (uint32_t i = 0; i < here; i += 32) {
-        const uint32_t word = S.bits[i / 32], in = here - i < 32u ? (1u << (here - i)) - 1u : 0xFFFFFFFFu;
-        const uint32_t alive = word & in, gone = ~word & in, before = (1u << lane) - 1u, no = slab_no(first + i + lane);
+      for (uint32_t i = 0; i < n_mine; i += 32) {
+        const uint32_t word = S.bits[i / 32], in = n_mine - i < 32u ? (1u << (n_mine - i)) - 1u : 0xFFFFFFFFu;
+        const uint32_t alive = word & in, gone = ~word & in, before = (1u << lane) - 1u, no = slab_no(i + lane);
         if ((alive >> lane) & 1u) S.live[n_live + __popc(alive & before)] = no;
         if ((gone >> lane) & 1u) S.dead[n_dead + __popc(gone & before)] = no;
         n_live += __popc(alive), n_dead += __popc(gone);
       }
       if (lane == 0) S.n_live = n_live, S.n_dead = n_dead;
     }
-    block_sync();
-  };
+  }
+  __syncthreads();
+  const uint32_t n_live = S.n_live;
 
   if (warp < 4) {
     if (LANE_IS_ROW) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // 384 threads of 168 registers: 256 x 216 + 128 x 72 are no more
-    for (uint32_t first = 0; first < n_mine; first += LIST) {
-      list_slabs(first);
-      const uint32_t n_live = S.n_live;
-      if (warp == 0 && elected()) {
-        for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
-          for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
-            // this block's slabs of the tile: all, or the first or second half of them
-            const uint32_t there = min(SLABS, n_live - g), half = (there + 1u) / 2u, from = FORM == PAIR ? g + rank * half : g;
-            const uint32_t count = FORM == PAIR ? (rank ? there - half : half) : there;
-            uint32_t y[Shape::slabs_here / 4], whole = 0u;  // of four slabs: the first one's rows, whether the others follow
+    if (warp == 0 && elected()) {
+      for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
+        for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
+          // this block's slabs of the tile: all, or the first or second half of them
+          const uint32_t there = min(SLABS, n_live - g), half = (there + 1u) / 2u, from = FORM == PAIR ? g + rank * half : g;
+          const uint32_t count = FORM == PAIR ? (rank ? there - half : half) : there;
+          uint32_t y[Shape::slabs_here / 4], whole = 0u;  // of four slabs: the first one's rows, whether the others follow
 #pragma unroll
-            for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
-              y[i] = 0u;
-              if (4u * i + 3u < count) {
-                y[i] = S.live[from + 4u * i] * SLAB;
-                if (S.live[from + 4u * i + 3u] * SLAB == y[i] + 3u * SLAB) whole |= 1u << i;
-              }
-            }
-            for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
-              if (!bar_wait(&S.empty[stage.at], stage.round ^ 1u, S)) {
-                failed = true;
-                break;
-              }
-              const uint32_t blocks = min(DEPTH, n_blocks - b), bar = at_first<FORM>(&S.full[stage.at]);
-              uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
-              if (FORM != PAIR || count) bar_expect_at<FORM>(bar, blocks * count * SLAB_BYTES);
-              else bar_arrive_at<FORM>(bar);
-              for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) {
-#pragma unroll
-                for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
-                  if ((whole >> i) & 1u) tma_load<FORM>(&wmap4, bar, at + 4u * i * SLAB_BYTES, k * BLOCK, y[i]);
-                  else
-                    for (uint32_t q = 4u * i; q < min(4u * i + 4u, count); ++q) tma_load<FORM>(&wmap, bar, at + q * SLAB_BYTES, k * BLOCK, S.live[from + q] * SLAB);
-                }
-              }
-              ++copied;
-              stage.next();
+          for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
+            y[i] = 0u;
+            if (4u * i + 3u < count) {
+              y[i] = S.live[from + 4u * i] * SLAB;
+              if (S.live[from + 4u * i + 3u] * SLAB == y[i] + 3u * SLAB) whole |= 1u << i;
             }
           }
-      } else if (warp == 3 && elected()) {
-        for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
-          for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y)
-            for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
-              if (!bar_wait(&S.empty[stage.at], stage.round ^ 1u, S)) {
-                failed = true;
-                break;
-              }
-              const uint32_t blocks = min(DEPTH, n_blocks - b), bar = at_first<FORM>(&S.full[stage.at]);
-              uint32_t at = tiles_at + stage.at * Shape::stage_bytes + Shape::slabs_here * SLAB_BYTES;
-              bar_expect_at<FORM>(bar, blocks * ROWS * BLOCK);
-              for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) tma_load<FORM>(&xmap, bar, at, k * BLOCK, (j * BLOCKS + rank) * ROWS);
-              ++copied;
-              stage.next();
+          for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
+            if (!bar_wait(&S.empty[stage.at], stage.round ^ 1u, S)) {
+              failed = true;
+              break;
             }
-      } else if (warp == 1 && rank == 0 && elected()) {  // (a pair's products are issued by its first block, for both)
-        for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
-          for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
-            // e4m3 x e4m3 into fp32, both K-major, 128 lanes (of each block)
-            const uint32_t there = min(SLABS, n_live - g), columns = FORM == FEW ? ROWS : FORM == WIDE ? there * SLAB : (there + 1u) / 2u * 2u * SLAB;
-            const uint32_t idesc = 1u << 4 | (columns >> 3) << 17 | (BLOCKS * 128u >> 4) << 24;
-            for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
-              const uint32_t at = tiles_at + stage.at * Shape::stage_bytes, d = S.tmem + buf.at * BUF;
-              const uint64_t w = tile_desc(at), x = tile_desc(at + Shape::slabs_here * SLAB_BYTES);
-              // the copies are early, mostly; the sums' place is what it waits for
-              if (!bar_wait(&S.full[stage.at], stage.round, S) || !bar_wait(FORM == PAIR ? &S.both_empty[buf.at] : &S.sums_empty[buf.at], buf.round ^ 1u, S)) {
-                failed = true;
-                break;
-              }
-              after_sync();
+            const uint32_t blocks = min(DEPTH, n_blocks - b), bar = at_first<FORM>(&S.full[stage.at]);
+            uint32_t at = tiles_at + stage.at * Shape::stage_bytes;
+            if (FORM != PAIR || count) bar_expect_at<FORM>(bar, blocks * count * SLAB_BYTES);
+            else bar_arrive_at<FORM>(bar);
+            for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) {
 #pragma unroll
-              for (uint32_t k = 0; k < DEPTH; ++k)
-                if (k == 0 || b + k < n_blocks) {
-#pragma unroll
-                  for (uint32_t i = 0; i < 4; ++i) {
-                    const uint32_t more = (k * Shape::block_bytes + 32u * i) >> 4;
-                    mma<FORM>(d + k * Shape::columns, (LANE_IS_ROW ? x : w) + more, (LANE_IS_ROW ? w : x) + more, idesc, i != 0);
-                  }
-                }
-              mma_commit<FORM>(&S.empty[stage.at]);
-              mma_commit<FORM>(&S.sums_full[buf.at]);
-              stage.next(), buf.next();
-            }
-          }
-      } else if (warp == 2) {
-        // A stage's scales are asked for AHEAD stages early, and their being there is one of the two things that sums_full waits for.
-        constexpr uint32_t AHEAD = SCALE_SLOTS - Shape::bufs;
-        const uint32_t total = (n_live + SLABS - 1) / SLABS * ((row_tiles + gridDim.y - 1 - blockIdx.y) / gridDim.y) * ((n_blocks + DEPTH - 1) / DEPTH);
-        uint32_t g = 0, j = blockIdx.y, b = 0;
-        for (uint32_t t = 0; t < total + AHEAD; ++t) {
-          if (t >= AHEAD) bar_wait_on(&S.sums_empty[buf.at], buf.round ^ 1u, S);
-          if (t < total) {
-            const uint32_t count = min(SLABS, n_live - g), r0 = (j * BLOCKS + rank) * ROWS;
-            for (uint32_t k = b; k < min(b + DEPTH, n_blocks); ++k) {
-              const uint32_t dst = smem_addr(scales + slot.at * Shape::slot_floats + (k - b) * Shape::block_floats);
-              const float* xp = A.xs + (size_t)k * A.xs_stride + r0;
-#pragma unroll
-              for (uint32_t i = 0; i < (ROWS + 31u) / 32u; ++i) {
-                const uint32_t c = i * 32u + lane;
-                if (c < ROWS && r0 + c < A.rows) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + c * 4u), "l"(xp + c) : "memory");
+              for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
+                if ((whole >> i) & 1u) tma_load<FORM>(&wmap4, bar, at + 4u * i * SLAB_BYTES, k * BLOCK, y[i]);
+                else
+                  for (uint32_t q = 4u * i; q < min(4u * i + 4u, count); ++q) tma_load<FORM>(&wmap, bar, at + q * SLAB_BYTES, k * BLOCK, S.live[from + q] * SLAB);
               }
-              if (lane < count)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + (ROWS + lane) * 4u),
-                             "l"(A.ws + (size_t)(S.live[g + lane] * SLAB / BLOCK) * A.ws_stride + k) : "memory");
             }
-            slot.next();
-            b += DEPTH;
-            if (b >= n_blocks) {
-              b = 0, j += gridDim.y;
-              if (j >= row_tiles) j = blockIdx.y, g += SLABS;
-            }
-          }
-          asm volatile("cp.async.commit_group;" ::: "memory");
-          if (t >= AHEAD) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
-            __syncwarp();
-            if (lane == 0) bar_arrive(&S.sums_full[buf.at]);
-            buf.next();
+            ++copied;
+            stage.next();
           }
         }
+    } else if (warp == 3 && elected()) {
+      for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
+        for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y)
+          for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
+            if (!bar_wait(&S.empty[stage.at], stage.round ^ 1u, S)) {
+              failed = true;
+              break;
+            }
+            const uint32_t blocks = min(DEPTH, n_blocks - b), bar = at_first<FORM>(&S.full[stage.at]);
+            uint32_t at = tiles_at + stage.at * Shape::stage_bytes + Shape::slabs_here * SLAB_BYTES;
+            bar_expect_at<FORM>(bar, blocks * ROWS * BLOCK);
+            for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) tma_load<FORM>(&xmap, bar, at, k * BLOCK, (j * BLOCKS + rank) * ROWS);
+            ++copied;
+            stage.next();
+          }
+    } else if (warp == 1 && rank == 0 && elected()) {  // (a pair's products are issued by its first block, for both)
+      for (uint32_t g = 0; g < n_live && !failed; g += SLABS)
+        for (uint32_t j = blockIdx.y; j < row_tiles && !failed; j += gridDim.y) {
+          // e4m3 x e4m3 into fp32, both K-major, 128 lanes (of each block)
+          const uint32_t there = min(SLABS, n_live - g), columns = FORM == FEW ? ROWS : FORM == WIDE ? there * SLAB : (there + 1u) / 2u * 2u * SLAB;
+          const uint32_t idesc = 1u << 4 | (columns >> 3) << 17 | (BLOCKS * 128u >> 4) << 24;
+          for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
+            const uint32_t at = tiles_at + stage.at * Shape::stage_bytes, d = S.tmem + buf.at * BUF;
+            const uint64_t w = tile_desc(at), x = tile_desc(at + Shape::slabs_here * SLAB_BYTES);
+            // the copies are early, mostly; the sums' place is what it waits for
+            if (!bar_wait(&S.full[stage.at], stage.round, S) || !bar_wait(FORM == PAIR ? &S.both_empty[buf.at] : &S.sums_empty[buf.at], buf.round ^ 1u, S)) {
+              failed = true;
+              break;
+            }
+            after_sync();
+#pragma unroll
+            for (uint32_t k = 0; k < DEPTH; ++k)
+              if (k == 0 || b + k < n_blocks) {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                  const uint32_t more = (k * Shape::block_bytes + 32u * i) >> 4;
+                  mma<FORM>(d + k * Shape::columns, (LANE_IS_ROW ? x : w) + more, (LANE_IS_ROW ? w : x) + more, idesc, i != 0);
+                }
+              }
+            mma_commit<FORM>(&S.empty[stage.at]);
+            mma_commit<FORM>(&S.sums_full[buf.at]);
+            stage.next(), buf.next();
+          }
+        }
+    } else if (warp == 2) {
+      // A stage's scales are asked for AHEAD stages early, and their being there is one of the two things that sums_full waits for.
+      constexpr uint32_t AHEAD = SCALE_SLOTS - Shape::bufs;
+      const uint32_t total = (n_live + SLABS - 1) / SLABS * ((row_tiles + gridDim.y - 1 - blockIdx.y) / gridDim.y) * ((n_blocks + DEPTH - 1) / DEPTH);
+      uint32_t g = 0, j = blockIdx.y, b = 0;
+      for (uint32_t t = 0; t < total + AHEAD; ++t) {
+        if (t >= AHEAD) bar_wait_on(&S.sums_empty[buf.at], buf.round ^ 1u, S);
+        if (t < total) {
+          const uint32_t count = min(SLABS, n_live - g), r0 = (j * BLOCKS + rank) * ROWS;
+          for (uint32_t k = b; k < min(b + DEPTH, n_blocks); ++k) {
+            const uint32_t dst = smem_addr(scales + slot.at * Shape::slot_floats + (k - b) * Shape::block_floats);
+            const float* xp = A.xs + (size_t)k * A.xs_stride + r0;
+#pragma unroll
+            for (uint32_t i = 0; i < (ROWS + 31u) / 32u; ++i) {
+              const uint32_t c = i * 32u + lane;
+              if (c < ROWS && r0 + c < A.rows) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + c * 4u), "l"(xp + c) : "memory");
+            }
+            if (lane < count)
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + (ROWS + lane) * 4u),
+                           "l"(A.ws + (size_t)(S.live[g + lane] * SLAB / BLOCK) * A.ws_stride + k) : "memory");
+          }
+          slot.next();
+          b += DEPTH;
+          if (b >= n_blocks) {
+            b = 0, j += gridDim.y;
+            if (j >= row_tiles) j = blockIdx.y, g += SLABS;
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (t >= AHEAD) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(&S.sums_full[buf.at]);
+          buf.next();
+        }
       }
-      __syncwarp();
-      block_sync();  // the lists are made anew
     }
+    __syncwarp();
     if (warp == 1 && rank == 0 && elected()) mma_commit<FORM>(&S.through);
     if ((warp == 0 || warp == 3) && copied)  // (the thread that was elected)
       asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at_first<FORM>(&S.copied[rank * 2u + (warp ? 1u : 0u)])), "r"(copied) : "memory");
@@ -596,201 +588,196 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
     const float minus_inf = -__int_as_float(0x7F800000), nan = __int_as_float(0x7FC00000);
     const uintptr_t begins = reinterpret_cast<uintptr_t>(logits) | A.row_stride * sizeof(T);  // rows begin at multiples of
     const bool by_units = (begins & 31u) == 0, by_words = (begins & 3u) == 0;                 // 32 or of four bytes
-    for (uint32_t first = 0; first < n_mine; first += LIST) {
-      list_slabs(first);
-      const uint32_t n_live = S.n_live;
-      // the slabs that no row may use
-      for (uint32_t i = warp - 4u; i < S.n_dead; i += ADD_WARPS) {
-        const uint32_t v = S.dead[i] * SLAB + lane;
-        if (v < A.V)
-          for (uint32_t r = blockIdx.y * BLOCKS + rank; r < A.rows; r += gridDim.y * BLOCKS) put(logits + (size_t)r * A.row_stride + v, minus_inf);
-      }
-      for (uint32_t g = 0; g < n_live; g += SLABS)
-        for (uint32_t j = blockIdx.y; j < row_tiles; j += gridDim.y) {
-          constexpr uint32_t COLS = Shape::columns / 2;      // of the tile, this warp's
-          constexpr uint32_t CHUNK = COLS < 32 ? COLS : 32;  // read from tensor memory in one go
-          constexpr uint32_t READS = DEPTH * COLS / CHUNK;   // of a stage; an even number
-          constexpr uint32_t FACTORS = LANE_IS_ROW ? 4 : DEPTH * COLS / 2;
-          const uint32_t count = n_live - g;                 // slabs that are there
-          const uint32_t mine = LANE_IS_ROW ? (count > half * 4u ? min(4u, count - half * 4u) : 0u) : quarter < count ? 1u : 0u;
-          // The masks' words are asked for now.  Where a lane is a row, a word for each of its slabs; else lane c holds row c's.
-          constexpr uint32_t WORDS = LANE_IS_ROW ? 4 : 1;
-          const uint32_t r0 = (j * BLOCKS + rank) * ROWS + (LANE_IS_ROW ? quarter * 32u : half * COLS);  // the first of the warp's rows
-          uint32_t word[WORDS];
+    // the slabs that no row may use
+    for (uint32_t i = warp - 4u; i < S.n_dead; i += ADD_WARPS) {
+      const uint32_t v = S.dead[i] * SLAB + lane;
+      if (v < A.V)
+        for (uint32_t r = blockIdx.y * BLOCKS + rank; r < A.rows; r += gridDim.y * BLOCKS) put(logits + (size_t)r * A.row_stride + v, minus_inf);
+    }
+    for (uint32_t g = 0; g < n_live; g += SLABS)
+      for (uint32_t j = blockIdx.y; j < row_tiles; j += gridDim.y) {
+        constexpr uint32_t COLS = Shape::columns / 2;      // of the tile, this warp's
+        constexpr uint32_t CHUNK = COLS < 32 ? COLS : 32;  // read from tensor memory in one go
+        constexpr uint32_t READS = DEPTH * COLS / CHUNK;   // of a stage; an even number
+        constexpr uint32_t FACTORS = LANE_IS_ROW ? 4 : DEPTH * COLS / 2;
+        const uint32_t count = n_live - g;                 // slabs that are there
+        const uint32_t mine = LANE_IS_ROW ? (count > half * 4u ? min(4u, count - half * 4u) : 0u) : quarter < count ? 1u : 0u;
+        // The masks' words are asked for now.  Where a lane is a row, a word for each of its slabs; else lane c holds row c's.
+        constexpr uint32_t WORDS = LANE_IS_ROW ? 4 : 1;
+        const uint32_t r0 = (j * BLOCKS + rank) * ROWS + (LANE_IS_ROW ? quarter * 32u : half * COLS);  // the first of the warp's rows
+        uint32_t word[WORDS];
 #pragma unroll
-          for (uint32_t i = 0; i < WORDS; ++i) {
-            word[i] = 0xFFFFFFFFu;
-            if (A.mask && (LANE_IS_ROW ? i < mine : mine && lane < COLS) && r0 + lane < A.rows)
-              word[i] = A.mask[(size_t)(r0 + lane) * A.mask_stride + S.live[g + (LANE_IS_ROW ? half * 4u + i : quarter)]];
+        for (uint32_t i = 0; i < WORDS; ++i) {
+          word[i] = 0xFFFFFFFFu;
+          if (A.mask && (LANE_IS_ROW ? i < mine : mine && lane < COLS) && r0 + lane < A.rows)
+            word[i] = A.mask[(size_t)(r0 + lane) * A.mask_stride + S.live[g + (LANE_IS_ROW ? half * 4u + i : quarter)]];
+        }
+        uint64_t sum[COLS / 2];
+#pragma unroll
+        for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = 0;
+        // Two pieces are on their way at a time; the first two of the next stage (if it is there) while the last two of this one are added.
+        float d[2][CHUNK];
+        const uint32_t lanes = S.tmem + (quarter * 32u << 16) + half * COLS;
+        auto read = [&](uint32_t r) { tmem_read<CHUNK>(lanes + buf.at * BUF + r * CHUNK / COLS * Shape::columns + r * CHUNK % COLS, d[r % 2]); };
+        auto stage_ready = [&] {
+          bar_wait_on(&S.sums_full[buf.at], buf.round, S);
+          after_sync();
+        };
+        stage_ready();
+        read(0), read(1);
+        for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
+          uint64_t by[FACTORS];  // the products of two scales
+          const float* sc = scales + slot.at * Shape::slot_floats;
+          if (LANE_IS_ROW) {  // a row's scale times its slabs'
+            const float x = sc[quarter * 32u + lane];
+            const float4 w = *reinterpret_cast<const float4*>(sc + ROWS + half * 4u);
+            by[0] = pair(x * w.x, x * w.x), by[1 % FACTORS] = pair(x * w.y, x * w.y);
+            by[2 % FACTORS] = pair(x * w.z, x * w.z), by[3 % FACTORS] = pair(x * w.w, x * w.w);
+          } else {  // the slab's scale times its rows'
+#pragma unroll
+            for (uint32_t k = 0; k < DEPTH; ++k) {
+              const float w = sc[k * Shape::block_floats + ROWS + quarter];
+#pragma unroll
+              for (uint32_t c = 0; c < COLS; c += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(sc + k * Shape::block_floats + half * COLS + c);
+                by[(k * COLS + c) / 2 % FACTORS] = pair(x.x * w, x.y * w), by[((k * COLS + c) / 2 + 1) % FACTORS] = pair(x.z * w, x.w * w);
+              }
+            }
           }
-          uint64_t sum[COLS / 2];
+          constexpr uint32_t PER = COLS / CHUNK;  // reads of a block of columns
+          auto add = [&](uint32_t r) {
+            if (r < PER || b + r / PER < n_blocks) {
 #pragma unroll
-          for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = 0;
-          // Two pieces are on their way at a time; the first two of the next stage (if it is there) while the last two of this one are added.
-          float d[2][CHUNK];
-          const uint32_t lanes = S.tmem + (quarter * 32u << 16) + half * COLS;
-          auto read = [&](uint32_t r) { tmem_read<CHUNK>(lanes + buf.at * BUF + r * CHUNK / COLS * Shape::columns + r * CHUNK % COLS, d[r % 2]); };
-          auto stage_ready = [&] {
-            bar_wait_on(&S.sums_full[buf.at], buf.round, S);
-            after_sync();
+              for (uint32_t c = 0; c < CHUNK; c += 2)
+                add_products(sum[(r % PER * CHUNK + c) / 2], d[r % 2][c], d[r % 2][c + 1], by[LANE_IS_ROW ? r : (r * CHUNK + c) / 2]);
+            }
           };
-          stage_ready();
-          read(0), read(1);
-          for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
-            uint64_t by[FACTORS];  // the products of two scales
-            const float* sc = scales + slot.at * Shape::slot_floats;
-            if (LANE_IS_ROW) {  // a row's scale times its slabs'
-              const float x = sc[quarter * 32u + lane];
-              const float4 w = *reinterpret_cast<const float4*>(sc + ROWS + half * 4u);
-              by[0] = pair(x * w.x, x * w.x), by[1 % FACTORS] = pair(x * w.y, x * w.y);
-              by[2 % FACTORS] = pair(x * w.z, x * w.z), by[3 % FACTORS] = pair(x * w.w, x * w.w);
-            } else {  // the slab's scale times its rows'
+          const bool more = b + DEPTH < n_blocks;
 #pragma unroll
-              for (uint32_t k = 0; k < DEPTH; ++k) {
-                const float w = sc[k * Shape::block_floats + ROWS + quarter];
-#pragma unroll
-                for (uint32_t c = 0; c < COLS; c += 4) {
-                  const float4 x = *reinterpret_cast<const float4*>(sc + k * Shape::block_floats + half * COLS + c);
-                  by[(k * COLS + c) / 2 % FACTORS] = pair(x.x * w, x.y * w), by[((k * COLS + c) / 2 + 1) % FACTORS] = pair(x.z * w, x.w * w);
-                }
+          for (uint32_t r = 0; r < READS; r += 2) {
+            tmem_read_done();
+            if (r + 2 == READS) {
+              before_sync();
+              __syncwarp();
+              if (lane == 0) {
+                if (FORM == PAIR) bar_arrive_at<FORM>(at_first<FORM>(&S.both_empty[buf.at]));
+                bar_arrive(&S.sums_empty[buf.at]);
               }
+              buf.next(), slot.next();
             }
-            constexpr uint32_t PER = COLS / CHUNK;  // reads of a block of columns
-            auto add = [&](uint32_t r) {
-              if (r < PER || b + r / PER < n_blocks) {
-#pragma unroll
-                for (uint32_t c = 0; c < CHUNK; c += 2)
-                  add_products(sum[(r % PER * CHUNK + c) / 2], d[r % 2][c], d[r % 2][c + 1], by[LANE_IS_ROW ? r : (r * CHUNK + c) / 2]);
-              }
-            };
-            const bool more = b + DEPTH < n_blocks;
-#pragma unroll
-            for (uint32_t r = 0; r < READS; r += 2) {
-              tmem_read_done();
-              if (r + 2 == READS) {
-                before_sync();
-                __syncwarp();
-                if (lane == 0) {
-                  if (FORM == PAIR) bar_arrive_at<FORM>(at_first<FORM>(&S.both_empty[buf.at]));
-                  bar_arrive(&S.sums_empty[buf.at]);
-                }
-                buf.next(), slot.next();
-              }
-              add(r);
-              if (r + 2 < READS) read(r + 2);
-              else if (more) stage_ready(), read(0);
-              add(r + 1);
-              if (r + 2 < READS) read(r + 3);
-              else if (more) read(1);
-            }
-          }
-          if (S.gave_up) {
-#pragma unroll
-            for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = pair(nan, nan);
-          }
-          if (LANE_IS_ROW && by_units && S.live[g + min(count, SLABS) - 1u] * SLAB + SLAB <= A.V) {
-            // a lane holds 32 tokens of a row for each slab, which are two (bf16) or four units of 32 bytes
-            if (r0 + lane < A.rows) {
-#pragma unroll
-              for (uint32_t i = 0; i < 4; ++i) {
-                if (i >= mine) break;
-                uint32_t* const to = reinterpret_cast<uint32_t*>(logits + (size_t)(r0 + lane) * A.row_stride + S.live[g + half * 4u + i] * SLAB);
-                const uint32_t allowed = word[i % WORDS];
-                uint32_t y[sizeof(T) * SLAB / 4];
-#pragma unroll
-                for (uint32_t c = 0; c < SLAB; c += 2) {
-                  const uint64_t two = sum[(i * SLAB + c) / 2 % (COLS / 2)];
-                  if (sizeof(T) == 2) y[c / 2] = two_bf16(part(two, 0), part(two, 1));
-                  else y[c % (sizeof(y) / 4)] = (uint32_t)two, y[(c + 1) % (sizeof(y) / 4)] = (uint32_t)(two >> 32);
-                }
-                if (allowed != 0xFFFFFFFFu) {
-                  if (sizeof(T) == 2) {
-#pragma unroll
-                    for (uint32_t c = 0; c < SLAB; c += 4) {
-                      const uint32_t bits = ((allowed >> c & 15u) * 0x00204081u & 0x01010101u) << 7;  // each bit the highest of a byte
-                      y[c / 2] = keep_pair(y[c / 2], bits, 0x9988u), y[c / 2 + 1] = keep_pair(y[c / 2 + 1], bits, 0xBBAAu);
-                    }
-                  } else {
-#pragma unroll
-                    for (uint32_t c = 0; c < SLAB; ++c) y[c % (sizeof(y) / 4)] = (allowed >> c) & 1u ? y[c % (sizeof(y) / 4)] : 0xFF800000u;
-                  }
-                }
-#pragma unroll
-                for (uint32_t q = 0; q < sizeof(y) / 4; q += 8)
-                  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + q), "r"(y[q]), "r"(y[q + 1]), "r"(y[q + 2]), "r"(y[q + 3]),
-                               "r"(y[q + 4]), "r"(y[q + 5]), "r"(y[q + 6]), "r"(y[q + 7])
-                               : "memory");
-              }
-            }
-          } else if (LANE_IS_ROW) {
-            const uint32_t rows_here = r0 < A.rows ? min(32u, A.rows - r0) : 0u;
-            uint32_t* const words = reinterpret_cast<uint32_t*>(own);
-            // One slab's code for all four, which has to be fetched for every tile: sums move down a slab's places each time.
-#pragma unroll 1
-            for (uint32_t i = 0; i < mine; ++i) {
-              if (!rows_here) break;
-              const uint32_t v0 = S.live[g + half * 4u + i] * SLAB;
-              uint64_t now[SLAB / 2];
-              const uint32_t allowed = word[0];
-#pragma unroll
-              for (uint32_t c = 0; c < SLAB / 2; ++c) now[c] = sum[c % (COLS / 2)];
-#pragma unroll
-              for (uint32_t c = SLAB / 2; c < COLS / 2; ++c) sum[(c - SLAB / 2) % (COLS / 2)] = sum[c];
-#pragma unroll
-              for (uint32_t k = 1; k < WORDS; ++k) word[k - 1] = word[k];
-              auto masked = [&](uint32_t c) { return (allowed >> c) & 1u ? part(now[c / 2], c % 2) : minus_inf; };
-              auto packed = [&](uint32_t c) {  // word c of the slab's row
-                return sizeof(T) == 4 ? __float_as_uint(masked(c % SLAB)) : two_bf16(masked(2 * c % SLAB), masked((2 * c + 1) % SLAB));
-              };
-              // rows that begin elsewhere: turned round in shared memory, 16 words of a row at a time, so that a warp writes them side by side
-              constexpr uint32_t TOKENS = TURN * 4 / sizeof(T);
-#pragma unroll
-              for (uint32_t t = 0; t < SLAB; t += TOKENS) {
-#pragma unroll
-                for (uint32_t c = 0; c < TURN; ++c) words[lane * (TURN + 1) + c] = packed(t * sizeof(T) / 4 + c);
-                __syncwarp();
-                if (by_words) {
-                  const uint32_t c = lane % TURN, v = v0 + t + c * (4 / sizeof(T));
-                  T* to = logits + (size_t)(r0 + lane / TURN) * A.row_stride + v;
-                  const bool all = v + 4 / sizeof(T) <= A.V, some = v < A.V;
-#pragma unroll
-                  for (uint32_t r = 0; r < 32u; r += 32u / TURN, to += 2 * A.row_stride) {
-                    const uint32_t y = words[(r + lane / TURN) * (TURN + 1) + c];
-                    if (r + lane / TURN < rows_here) {
-                      if (all) *reinterpret_cast<uint32_t*>(to) = y;
-                      else if (some) *reinterpret_cast<uint16_t*>(to) = (uint16_t)y;
-                    }
-                  }
-                } else {  // bf16
-                  const uint32_t v = v0 + t + lane;
-                  T* to = logits + (size_t)r0 * A.row_stride + v;
-#pragma unroll
-                  for (uint32_t r = 0; r < 32u; ++r, to += A.row_stride) {
-                    const uint16_t y = reinterpret_cast<const uint16_t*>(words + r * (TURN + 1))[lane];
-                    if (r < rows_here && v < A.V) *reinterpret_cast<uint16_t*>(to) = y;
-                  }
-                }
-                __syncwarp();
-              }
-            }
-          } else if (mine && r0 < A.rows) {
-            const uint32_t v = S.live[g + quarter] * SLAB + lane;
-            T* to = logits + (size_t)r0 * A.row_stride + v;
-#pragma unroll 1
-            for (uint32_t c0 = 0; c0 < COLS && r0 + c0 < A.rows; c0 += 8) {
-#pragma unroll
-              for (uint32_t c = 0; c < 8; ++c, to += A.row_stride) {
-                const uint32_t m = __shfl_sync(0xFFFFFFFFu, word[0], c0 + c);
-                const float y = (m >> lane) & 1u ? part(sum[c / 2], c % 2) : minus_inf;
-                if (r0 + c0 + c < A.rows && v < A.V) put(to, y);
-              }
-#pragma unroll
-              for (uint32_t c = 4; c < COLS / 2; ++c) sum[c - 4] = sum[c];
-            }
+            add(r);
+            if (r + 2 < READS) read(r + 2);
+            else if (more) stage_ready(), read(0);
+            add(r + 1);
+            if (r + 2 < READS) read(r + 3);
+            else if (more) read(1);
           }
         }
-      block_sync();
-    }
+        if (S.gave_up) {
+#pragma unroll
+          for (uint32_t c = 0; c < COLS / 2; ++c) sum[c] = pair(nan, nan);
+        }
+        if (LANE_IS_ROW && by_units && S.live[g + min(count, SLABS) - 1u] * SLAB + SLAB <= A.V) {
+          // a lane holds 32 tokens of a row for each slab, which are two (bf16) or four units of 32 bytes
+          if (r0 + lane < A.rows) {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+              if (i >= mine) break;
+              uint32_t* const to = reinterpret_cast<uint32_t*>(logits + (size_t)(r0 + lane) * A.row_stride + S.live[g + half * 4u + i] * SLAB);
+              const uint32_t allowed = word[i % WORDS];
+              uint32_t y[sizeof(T) * SLAB / 4];
+#pragma unroll
+              for (uint32_t c = 0; c < SLAB; c += 2) {
+                const uint64_t two = sum[(i * SLAB + c) / 2 % (COLS / 2)];
+                if (sizeof(T) == 2) y[c / 2] = two_bf16(part(two, 0), part(two, 1));
+                else y[c % (sizeof(y) / 4)] = (uint32_t)two, y[(c + 1) % (sizeof(y) / 4)] = (uint32_t)(two >> 32);
+              }
+              if (allowed != 0xFFFFFFFFu) {
+                if (sizeof(T) == 2) {
+#pragma unroll
+                  for (uint32_t c = 0; c < SLAB; c += 4) {
+                    const uint32_t bits = ((allowed >> c & 15u) * 0x00204081u & 0x01010101u) << 7;  // each bit the highest of a byte
+                    y[c / 2] = keep_pair(y[c / 2], bits, 0x9988u), y[c / 2 + 1] = keep_pair(y[c / 2 + 1], bits, 0xBBAAu);
+                  }
+                } else {
+#pragma unroll
+                  for (uint32_t c = 0; c < SLAB; ++c) y[c % (sizeof(y) / 4)] = (allowed >> c) & 1u ? y[c % (sizeof(y) / 4)] : 0xFF800000u;
+                }
+              }
+#pragma unroll
+              for (uint32_t q = 0; q < sizeof(y) / 4; q += 8)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + q), "r"(y[q]), "r"(y[q + 1]), "r"(y[q + 2]), "r"(y[q + 3]),
+                             "r"(y[q + 4]), "r"(y[q + 5]), "r"(y[q + 6]), "r"(y[q + 7])
+                             : "memory");
+            }
+          }
+        } else if (LANE_IS_ROW) {
+          const uint32_t rows_here = r0 < A.rows ? min(32u, A.rows - r0) : 0u;
+          uint32_t* const words = reinterpret_cast<uint32_t*>(own);
+          // One slab's code for all four, which has to be fetched for every tile: sums move down a slab's places each time.
+#pragma unroll 1
+          for (uint32_t i = 0; i < mine; ++i) {
+            if (!rows_here) break;
+            const uint32_t v0 = S.live[g + half * 4u + i] * SLAB;
+            uint64_t now[SLAB / 2];
+            const uint32_t allowed = word[0];
+#pragma unroll
+            for (uint32_t c = 0; c < SLAB / 2; ++c) now[c] = sum[c % (COLS / 2)];
+#pragma unroll
+            for (uint32_t c = SLAB / 2; c < COLS / 2; ++c) sum[(c - SLAB / 2) % (COLS / 2)] = sum[c];
+#pragma unroll
+            for (uint32_t k = 1; k < WORDS; ++k) word[k - 1] = word[k];
+            auto masked = [&](uint32_t c) { return (allowed >> c) & 1u ? part(now[c / 2], c % 2) : minus_inf; };
+            auto packed = [&](uint32_t c) {  // word c of the slab's row
+              return sizeof(T) == 4 ? __float_as_uint(masked(c % SLAB)) : two_bf16(masked(2 * c % SLAB), masked((2 * c + 1) % SLAB));
+            };
+            // rows that begin elsewhere: turned round in shared memory, 16 words of a row at a time, so that a warp writes them side by side
+            constexpr uint32_t TOKENS = TURN * 4 / sizeof(T);
+#pragma unroll
+            for (uint32_t t = 0; t < SLAB; t += TOKENS) {
+#pragma unroll
+              for (uint32_t c = 0; c < TURN; ++c) words[lane * (TURN + 1) + c] = packed(t * sizeof(T) / 4 + c);
+              __syncwarp();
+              if (by_words) {
+                const uint32_t c = lane % TURN, v = v0 + t + c * (4 / sizeof(T));
+                T* to = logits + (size_t)(r0 + lane / TURN) * A.row_stride + v;
+                const bool all = v + 4 / sizeof(T) <= A.V, some = v < A.V;
+#pragma unroll
+                for (uint32_t r = 0; r < 32u; r += 32u / TURN, to += 2 * A.row_stride) {
+                  const uint32_t y = words[(r + lane / TURN) * (TURN + 1) + c];
+                  if (r + lane / TURN < rows_here) {
+                    if (all) *reinterpret_cast<uint32_t*>(to) = y;
+                    else if (some) *reinterpret_cast<uint16_t*>(to) = (uint16_t)y;
+                  }
+                }
+              } else {  // bf16
+                const uint32_t v = v0 + t + lane;
+                T* to = logits + (size_t)r0 * A.row_stride + v;
+#pragma unroll
+                for (uint32_t r = 0; r < 32u; ++r, to += A.row_stride) {
+                  const uint16_t y = reinterpret_cast<const uint16_t*>(words + r * (TURN + 1))[lane];
+                  if (r < rows_here && v < A.V) *reinterpret_cast<uint16_t*>(to) = y;
+                }
+              }
+              __syncwarp();
+            }
+          }
+        } else if (mine && r0 < A.rows) {
+          const uint32_t v = S.live[g + quarter] * SLAB + lane;
+          T* to = logits + (size_t)r0 * A.row_stride + v;
+#pragma unroll 1
+          for (uint32_t c0 = 0; c0 < COLS && r0 + c0 < A.rows; c0 += 8) {
+#pragma unroll
+            for (uint32_t c = 0; c < 8; ++c, to += A.row_stride) {
+              const uint32_t m = __shfl_sync(0xFFFFFFFFu, word[0], c0 + c);
+              const float y = (m >> lane) & 1u ? part(sum[c / 2], c % 2) : minus_inf;
+              if (r0 + c0 + c < A.rows && v < A.V) put(to, y);
+            }
+#pragma unroll
+            for (uint32_t c = 4; c < COLS / 2; ++c) sum[c - 4] = sum[c];
+          }
+        }
+      }
   }
   // Nothing is in flight when a block ends: every copy has landed (a stage that not all the copying threads came to fill is filled up
   // first), every product is through, and nobody writes to a block's barriers any more.
@@ -865,8 +852,9 @@ fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, int dev, uint32
   uint32_t split = 1, least = 0xFFFFFFFFu;
   for (uint32_t y = 1; y <= row_tiles && y <= most; ++y) {
     const uint32_t x = std::min(most / y, slabs), each = (slabs + x - 1) / x, turns = (row_tiles + y - 1) / y;
-    if (each * turns < least) least = each * turns, split = y;
+    if (each <= LIST && (uint64_t)each * turns < least) least = each * turns, split = y;
   }
+  if (least == 0xFFFFFFFFu) return refuse("the vocabulary is too large for this device's number of SMs");
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(std::min(most / split, slabs) * BLOCKS, split), cfg.blockDim = dim3(HEAD_THREADS), cfg.dynamicSmemBytes = Shape::smem, cfg.stream = st;
   cudaLaunchAttribute at[2];
@@ -925,7 +913,7 @@ extern "C" fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_s
                                       size_t row_stride_elems, void* stream) {
   if (!hidden_dev || !hidden_scales_dev || !weight_dev || !weight_scales_dev || !logits_dev) return refuse("NULL argument");
   if (dtype != FMT_BF16 && dtype != FMT_FP32) return refuse("unknown dtype");
-  if (V == 0 || V > (1u << 24) || K == 0 || K > (1u << 20) || rows > (1u << 24)) return refuse("rows, V or K out of range");
+  if (V == 0 || V > MOST_TOKENS || K == 0 || K > (1u << 20) || rows > (1u << 24)) return refuse("rows, V or K out of range");
   if (hidden_stride < K || weight_stride < K || hidden_scale_stride < rows || weight_scale_stride < (K + BLOCK - 1) / BLOCK ||
       row_stride_elems < V || (mask_dev && mask_stride_words < (V + 31) / 32))
     return refuse("a stride is too small");

@@ -192,8 +192,8 @@ def test_rows_begin_at_any_address(n, offset, row_pad, dtype):
 
 
 @gpu
-@pytest.mark.parametrize("n,V,mask", [(3, 2600000, "few"), (3, 2600000, "none"), (130, 1300000, "few"), (130, 1300000, "mixed")])
-def test_more_slabs_than_a_list_holds(n, V, mask):
+@pytest.mark.parametrize("n,V,mask", [(3, 1 << 20, "few"), (3, 1 << 20, "none"), (130, 1 << 20, "few"), (130, 1000001, "mixed"), (700, 1 << 20, "few")])
+def test_the_largest_vocabularies(n, V, mask):
     h = Head(n, V, 16, mask, "bf16", seed=n)
     h.call()
     h.check()
@@ -339,7 +339,7 @@ def test_refusals():
         refused(h, **{name: None})
     refused(h, dtype=2)
     refused(h, V=0)
-    refused(h, V=(1 << 24) + 1)
+    refused(h, V=(1 << 20) + 1)
     refused(h, K=0)
     refused(h, K=(1 << 20) + 16)
     refused(h, rows=(1 << 24) + 1)
