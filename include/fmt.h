@@ -461,7 +461,7 @@ fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_stride, cons
  *                     -1 where fewer are allowed.  With n_top = 1 these are the greedy tokens, as fmt_state_advance takes them
  *   top_logprobs_dev  [rows][n_top] their ln p, -inf beside -1
  *   status_dev        [rows] int32: FMT_OK, or FMT_ERR_INVALID_ARG: a given token is not in [-1, V) (its log probability is NaN,
- *                     the others stand), or the temperature is not a positive finite number, or an allowed logit is NaN or
+ *                     the others stand), or the temperature is not a positive normal number (2^-126 or more, finite), or an allowed logit is NaN or
  *                     +inf (all the row's outputs are NaN, its alternatives -1)
  * A row without an allowed token: log probabilities -inf, M and ln S -inf, entropy 0, alternatives -1.
  */

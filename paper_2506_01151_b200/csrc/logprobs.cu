@@ -644,7 +644,7 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
   a = J.warps[0];
 
   const float nan = __int_as_float(0x7FC00000);
-  const bool bad = a.s != a.s || !(temperature > 0.0f && temperature < INF);
+  const bool bad = a.s != a.s || !(temperature >= 0x1p-126f && temperature < INF);  // (below, log2(e) / T overflows)
   const float ln = bad ? nan : logf(a.s);  // (-inf of nothing)
   auto logprob = [&](float x) { return bad ? nan : x == -INF ? -INF : (x - a.m) * inv - ln; };
   const bool wrong = token < -1 || token >= (int64_t)R.V;

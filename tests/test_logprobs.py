@@ -285,6 +285,19 @@ def test_extreme_temperatures_and_logits(scale, shift, temperature):
 
 
 @gpu
+@pytest.mark.parametrize("mask", ["none", "mixed"])
+def test_temperatures_that_are_not_normal_numbers(mask):
+    torch = torch_()
+    i = Inputs(4, 700, "fp32", mask, seed=2)
+    i.temperature[0], i.temperature[1], i.temperature[2] = 1.1754942e-38, 1e-40, 2.0 ** -126  # the first is just below
+    i.allow[:, 5] = True
+    out = i.forward()
+    assert out["status"][:4].tolist() == [fmt.ERR_INVALID_ARG, fmt.ERR_INVALID_ARG, fmt.FMT_OK, fmt.FMT_OK]
+    assert bool(torch.isnan(out["logprobs"][:2]).all()) and bool((out["ids"][:2] == -1).all()) and bool(torch.isnan(out["norm"][:2]).all())
+    assert float(out["tops"][2, 0]) == 0.0 and not bool(torch.isnan(out["logprobs"][2]).any())
+
+
+@gpu
 @pytest.mark.parametrize("n_tokens", [0, 1, 32])
 @pytest.mark.parametrize("with_g,with_h", [(True, False), (False, True), (False, False)])
 def test_gradients_that_are_not_given(n_tokens, with_g, with_h):
