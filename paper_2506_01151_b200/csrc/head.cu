@@ -378,16 +378,22 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
   const bool whole = A.mask && n_slabs <= ALL_SLABS && (uint64_t)n_slabs * A.rows <= ALL_WORDS && n_slabs > parties && n_mine < LIST;
   // The block's slabs that some row may use, and the others.
   if (whole) {
-    // lanes are slabs: their words lie side by side
-    for (uint32_t i = warp; i < (n_slabs + 31u) / 32u; i += HEAD_THREADS / 32) {
-      const uint32_t no = i * 32u + lane;
-      uint32_t any = 0u;
-      if (no < n_slabs) {
+    // lanes are slabs, whose words lie side by side; four times 32 slabs and eight rows are asked for at a time
+    constexpr uint32_t AT_ONCE = 4, WARPS = HEAD_THREADS / 32;
+    for (uint32_t i = warp; i < (n_slabs + 31u) / 32u; i += AT_ONCE * WARPS) {
+      uint32_t any[AT_ONCE] = {};
 #pragma unroll 8
-        for (uint32_t r = 0; r < A.rows; ++r) any |= A.mask[(size_t)r * A.mask_stride + no];
+      for (uint32_t r = 0; r < A.rows; ++r)
+#pragma unroll
+        for (uint32_t u = 0; u < AT_ONCE; ++u) {
+          const uint32_t no = (i + u * WARPS) * 32u + lane;
+          if (no < n_slabs) any[u] |= A.mask[(size_t)r * A.mask_stride + no];
+        }
+#pragma unroll
+      for (uint32_t u = 0; u < AT_ONCE; ++u) {
+        const uint32_t word = __ballot_sync(0xFFFFFFFFu, any[u] != 0u);
+        if (lane == 0 && i + u * WARPS < (n_slabs + 31u) / 32u) S.bits[i + u * WARPS] = word;
       }
-      const uint32_t word = __ballot_sync(0xFFFFFFFFu, any != 0u);
-      if (lane == 0) S.bits[i] = word;
     }
     __syncthreads();
     if (warp == 0) {  // the slabs that some row may use are dealt out among the blocks as all are otherwise
