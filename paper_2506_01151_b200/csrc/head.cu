@@ -470,14 +470,11 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
           // this block's slabs of the tile: all, or the first or second half of them
           const uint32_t there = min(SLABS, n_live - g), half = (there + 1u) / 2u, from = FORM == PAIR ? g + rank * half : g;
           const uint32_t count = FORM == PAIR ? (rank ? there - half : half) : there;
-          uint32_t y[Shape::slabs_here / 4], whole = 0u;  // of four slabs: the first one's rows, whether the others follow
+          uint32_t y[Shape::slabs_here], whole = 0u;  // the slabs' rows, and of four slabs, whether they follow one another
 #pragma unroll
-          for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
-            y[i] = 0u;
-            if (4u * i + 3u < count) {
-              y[i] = S.live[from + 4u * i] * SLAB;
-              if (S.live[from + 4u * i + 3u] * SLAB == y[i] + 3u * SLAB) whole |= 1u << i;
-            }
+          for (uint32_t i = 0; i < Shape::slabs_here; ++i) {
+            y[i] = i < count ? S.live[from + i] * SLAB : 0u;
+            if (i % 4u == 3u && i < count && y[i] == y[i - i % 4u] + 3u * SLAB) whole |= 1u << i / 4u;
           }
           for (uint32_t b = 0; b < n_blocks; b += DEPTH) {
             if (!bar_wait(&S.empty[stage.at], stage.round ^ 1u, S)) {
@@ -491,9 +488,13 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
             for (uint32_t k = b; k < b + blocks; ++k, at += Shape::block_bytes) {
 #pragma unroll
               for (uint32_t i = 0; i < Shape::slabs_here / 4; ++i) {
-                if ((whole >> i) & 1u) tma_load<FORM>(&wmap4, bar, at + 4u * i * SLAB_BYTES, k * BLOCK, y[i]);
-                else
-                  for (uint32_t q = 4u * i; q < min(4u * i + 4u, count); ++q) tma_load<FORM>(&wmap, bar, at + q * SLAB_BYTES, k * BLOCK, S.live[from + q] * SLAB);
+                if ((whole >> i) & 1u) {
+                  tma_load<FORM>(&wmap4, bar, at + 4u * i * SLAB_BYTES, k * BLOCK, y[4u * i]);
+                } else {
+#pragma unroll
+                  for (uint32_t q = 4u * i; q < 4u * i + 4u; ++q)
+                    if (q < count) tma_load<FORM>(&wmap, bar, at + q * SLAB_BYTES, k * BLOCK, y[q]);
+                }
               }
             }
             ++copied;
