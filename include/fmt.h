@@ -476,8 +476,9 @@ fmt_status fmt_token_logprobs(const void* logits_dev, fmt_dtype dtype, uint32_t 
  * The gradient of fmt_token_logprobs with respect to the logits, for a loss whose derivatives by a row's log probabilities
  * and entropy are grad_logprobs_dev and grad_entropy_dev (either may be NULL: zeros):
  *   grad[v] = (sum over given tokens t equal to v: g_t - p(v) * sum over t: g_t - g_H * p(v) * (ln p(v) + H)) / T
- * and 0 where the token is not allowed or its logit is -inf.  The g_t of a given token does not count where it is -1, out of
- * range, or its log probability is -inf.  A token given twice counts twice.
+ * and 0 where the token is not allowed or its logit is -inf, whatever the derivatives are.  (A p(v) below 2^-149 counts as 0, and so
+ * does what it is multiplied with; 1 / T comes last.)  The g_t of a given token does not count where it is -1, out of range, or its
+ * log probability is -inf.  A token given twice counts twice.
  *   logits .. n_tokens  as in the forward call
  *   norm_dev            the forward call's norm_dev; entropy_dev its entropy_dev (needed with grad_entropy_dev only)
  *   grad_logits_dev     [rows][V] of the logits' dtype, rows grad_stride_elems apart; it may be the logits themselves, with their

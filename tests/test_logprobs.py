@@ -297,6 +297,60 @@ def test_temperatures_that_are_not_normal_numbers(mask):
     assert float(out["tops"][2, 0]) == 0.0 and not bool(torch.isnan(out["logprobs"][2]).any())
 
 
+def check_gradient_of_any_size(i, out):
+    """The gradient where 1 / T or the gradients that come in are large: a p that fp32 does not hold (below 2^-149) counts as 0, and what is
+    left of one that it holds as a denormal is off by half of 2^-149, each times what it is multiplied with."""
+    want = i.reference()
+    norm, T = want["norm"], i.temperature.double()[:, None]
+    lp = ((i.logits.double() - norm[:, :1]) / T - norm[:, 1:]).abs().nan_to_num(0, 0, 0).clamp(max=104)
+    H = want["entropy"].abs()[:, None]
+    less = 2.0 ** -149 * (i.g.double().abs().sum(1, keepdim=True) + i.gh.double().abs()[:, None] * (lp + H + 2)) / T
+    allow = i.allow if i.masked else torch_().ones_like(i.allow)
+    want["tol"]["grad"] = want["tol"]["grad"] + torch_().where(allow, less, 0.0)
+    grad = i.backward(out)
+    check_backward(i, grad, want)
+    assert bool((grad[~allow] == 0).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("mask", ["none", "mixed", "few"])
+@pytest.mark.parametrize("temperature,g,gh", [(2.0 ** -126, 0.5, 1.0), (1e-37, 0.5, 1.0), (1e-37, 0.5, -8.0), (1e-30, 1.0, 1.0), (1e-12, 1.0, 1.0),
+                                              (2e-6, 1.0, 1e18), (1.0, 1.0, 1e28), (1.0, 1e33, 1e33), (0.7, 1e30, 0.0), (1e30, 1e33, -1e33)])
+def test_gradients_that_are_large(temperature, g, gh, mask, dtype):
+    """1 / T, or a gradient by the entropy, that is large: 0 where nothing is allowed or p is 0, and no overflow on the way to a number."""
+    torch = torch_()
+    i = Inputs(6, 5003, dtype, mask, offset=3, n_tokens=3, seed=11)
+    i.temperature[:] = temperature
+    if mask != "few":
+        i.allow[:, :4] = True
+        i.logits[3:, 2] = 20.0  # the likeliest by far
+    i.g.clamp_(-1, 1).mul_(g)
+    i.gh.clamp_(-1, 1).mul_(gh)
+    i.tokens[3:, 0] = 2
+    i.tokens[4:, 1] = 2
+    check_gradient_of_any_size(i, i.forward())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("by", ["g", "gh"])
+def test_gradients_that_are_not_finite_reach_allowed_tokens_only(by, value, dtype):
+    torch = torch_()
+    i = Inputs(4, 3001, dtype, "mixed", offset=1, seed=12)
+    i.allow[:, :8] = True
+    i.tokens[:] = torch.tensor([1, 6], dtype=torch.int32, device=DEV)
+    i.logits[:, 10:40] = -float("inf")
+    out = i.forward()
+    getattr(i, by)[1] = value
+    grad = i.backward(out)
+    off = ~i.allow | (i.logits == -torch.inf)
+    assert bool((grad[off] == 0).all())
+    assert not bool(torch.isfinite(grad[1][~off[1]]).any())
+    assert bool(torch.isfinite(grad[[0, 2, 3]]).all())
+
+
 @gpu
 @pytest.mark.parametrize("n_tokens", [0, 1, 32])
 @pytest.mark.parametrize("with_g,with_h", [(True, False), (False, True), (False, False)])
