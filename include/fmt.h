@@ -438,12 +438,16 @@ fmt_status fmt_quantize_blocks(const void* x_dev, fmt_dtype dtype, uint32_t rows
  *   hidden_stride, weight_stride  bytes from row to row, at least K, multiples of 16; both arrays 16-byte aligned
  *   mask_dev     [rows][mask_stride_words] packed masks (fmt_fill_mask), or NULL: every token is allowed
  * K and V at most 2^20, rows at most 2^24.  Every wait inside the kernel is a poll with an iteration limit; should one run out,
- * the logits that are not computed become NaN.
+ * nothing hangs, the logits that are not computed become NaN, and the next call is one like any other.
  */
 fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_stride, const float* hidden_scales_dev, size_t hidden_scale_stride,
                            const uint8_t* weight_dev, size_t weight_stride, const float* weight_scales_dev, size_t weight_scale_stride,
                            uint32_t rows, uint32_t V, uint32_t K, const uint32_t* mask_dev, size_t mask_stride_words,
                            void* logits_dev, fmt_dtype dtype, size_t row_stride_elems, void* stream);
+
+/* At most `polls` polls to a wait inside fmt_head_logits, from the next call or capture on: for the whole process, 2^18 (some 400 ms)
+ * unless set, and never more.  0: no wait lasts, every allowed logit is NaN.  (A test aid, as fmt_state_set_wait_limit.) */
+fmt_status fmt_head_set_wait_limit(uint32_t polls);
 
 /*
  * Log probabilities under the mask: of given tokens, of the likeliest ones, and the entropy.  A row's distribution is

@@ -24,7 +24,7 @@ EXPORTS = [
     "fmt_state_create", "fmt_state_destroy", "fmt_state_reset", "fmt_state_advance", "fmt_state_forced_bytes", "fmt_fill_mask",
     "fmt_apply_mask", "fmt_fill_and_apply", "fmt_state_cache_clear", "fmt_state_ci_cache_clear", "fmt_state_set_wait_limit", "fmt_state_copy_counters", "fmt_state_query", "fmt_state_copy_chart", "fmt_get_stats",
     "fmt_state_set_profiling", "fmt_state_read_profile", "fmt_state_read_profile_series", "fmt_fill_mask_noalloc",
-    "fmt_quantize_blocks", "fmt_head_logits", "fmt_token_logprobs", "fmt_token_logprobs_backward", "fmt_last_error",
+    "fmt_quantize_blocks", "fmt_head_logits", "fmt_head_set_wait_limit", "fmt_token_logprobs", "fmt_token_logprobs_backward", "fmt_last_error",
 ]
 
 
@@ -111,6 +111,7 @@ def lib():
         L.fmt_fill_mask_noalloc.argtypes = [vp, vp, vp, u32, vp, vp, vp]
         L.fmt_quantize_blocks.argtypes = [vp, C.c_int, u32, u32, sz, u32, vp, sz, vp, sz, vp]
         L.fmt_head_logits.argtypes = [vp, sz, vp, sz, vp, sz, vp, sz, u32, u32, u32, vp, sz, vp, C.c_int, sz, vp]
+        L.fmt_head_set_wait_limit.argtypes = [u32]
         L.fmt_token_logprobs.argtypes = [vp, C.c_int, u32, u32, sz, vp, sz, vp, vp, u32, u32, vp, vp, vp, vp, vp, vp, vp]
         L.fmt_token_logprobs_backward.argtypes = [vp, C.c_int, u32, u32, sz, vp, sz, vp, vp, u32, vp, vp, vp, vp, vp, sz, vp]
         L.fmt_last_error.restype = C.c_char_p
@@ -399,6 +400,11 @@ def head_logits(hidden_dev, hidden_scales_dev, weight_dev, weight_scales_dev, lo
     rs = V if row_stride is None else row_stride
     _check(lib().fmt_head_logits(_ptr(hidden_dev), hs, _ptr(hidden_scales_dev), hss, _ptr(weight_dev), ws, _ptr(weight_scales_dev), wss,
                                  rows, V, K, _ptr(mask_dev), ms, _ptr(logits_dev), dtype, rs, _ptr(stream)))
+
+
+def head_set_wait_limit(polls: int = 0xFFFFFFFF):
+    """fmt_head_set_wait_limit: polls to a wait inside head_logits, at most; without an argument as many as there may be."""
+    _check(lib().fmt_head_set_wait_limit(polls))
 
 
 def token_logprobs(logits_dev, dtype: int, rows: int, V: int, tokens_dev=None, n_tokens: int = 0, logprobs_dev=None, norm_dev=None,

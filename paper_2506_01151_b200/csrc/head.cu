@@ -119,6 +119,7 @@ constexpr uint32_t ALL_WORDS = 32768; // of the masks then
 constexpr uint32_t SCALE_SLOTS = 8;
 constexpr uint32_t SLAB_BYTES = SLAB * BLOCK;
 constexpr uint32_t WAIT_POLLS = 1u << 18;  // of 2,900 cycles, the time after which a wait for nothing comes back
+std::atomic<uint32_t> wait_polls{WAIT_POLLS};
 constexpr uint32_t WIDE_ROWS = 128;        // the M side's
 constexpr uint32_t TURN = 16;              // words of a row that a warp turns round in shared memory on their way out
 
@@ -151,11 +152,12 @@ struct HeadArgs {
   size_t mask_stride;
   void* logits;
   size_t row_stride;
+  uint32_t polls;  // of a wait, at most
 };
 
 struct HeadShared {
   uint64_t full[6], empty[6], sums_full[4], sums_empty[4], both_empty[4], through;
-  uint32_t tmem, n_live, n_dead, copied[4];  // (copied: stages, by the copying warps of this block and the other one)
+  uint32_t tmem, n_live, n_dead, polls, copied[4];  // (copied: stages, by the copying warps of this block and the other one)
   volatile uint32_t gave_up;
   uint32_t bits[ALL_SLABS / 32], upto[ALL_SLABS / 32];
   uint32_t live[LIST], dead[LIST];
@@ -199,22 +201,22 @@ __device__ __forceinline__ uint32_t pair_rank() {
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Waits until the barrier's phase of this parity is over.  False: given up, here or by another warp of the block.
+// Waits until the barrier's phase of this parity is over.  False: given up, here or by another warp of the block.  Who has given up asks for
+// no copy or product any more and arrives at no barrier of scales or sums: a phase that is over is so by whom it waits for, and nothing is
+// overwritten that another warp, or the other block of a pair (which may not have given up), still reads.  What the block writes from
+// then on is NaN.  (Looking at gave_up before each product instead takes 5 % in pairs: 2,048 rows 1,065 us, and so 1,013.)
 __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, HeadShared& S) {
   if (bar_test(b, parity)) return true;
-  for (uint32_t i = 0; i < WAIT_POLLS && !S.gave_up; ++i)
+  for (uint32_t i = 0; !S.gave_up && i < S.polls; ++i)
     if (bar_test(b, parity)) return true;
   S.gave_up = 1u;
   return false;
 }
 // The same for a whole warp, which goes on either way and looks at gave_up when it is through with a tile.
-__device__ __forceinline__ void bar_wait_on(uint64_t* b, uint32_t parity, HeadShared& S) {
-  if (!bar_test(b, parity)) {
-    uint32_t i = 0;
-    while (!bar_test(b, parity) && !S.gave_up)
-      if (++i == WAIT_POLLS) S.gave_up = 1u;
-  }
+__device__ __forceinline__ bool bar_wait_on(uint64_t* b, uint32_t parity, HeadShared& S) {
+  const bool there = bar_wait(b, parity, S);
   __syncwarp();
+  return there;
 }
 __device__ __forceinline__ void bar_drain(uint64_t* b, uint32_t parity) {  // the same after giving up, for what is in flight
   for (uint32_t i = 0; i < WAIT_POLLS && !bar_test(b, parity); ++i) {}
@@ -342,7 +344,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
     for (uint32_t i = 0; i < Shape::stages; ++i) bar_init(&S.full[i], 2 * BLOCKS), bar_init(&S.empty[i], 1);
     for (uint32_t i = 0; i < Shape::bufs; ++i) bar_init(&S.sums_full[i], 2), bar_init(&S.sums_empty[i], ADD_WARPS), bar_init(&S.both_empty[i], 2 * ADD_WARPS);
     bar_init(&S.through, 1);
-    S.gave_up = 0u, S.copied[0] = S.copied[1] = S.copied[2] = S.copied[3] = 0u;
+    S.polls = A.polls, S.gave_up = A.polls == 0u, S.copied[0] = S.copied[1] = S.copied[2] = S.copied[3] = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -551,7 +553,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
       const uint32_t total = (n_live + SLABS - 1) / SLABS * ((row_tiles + gridDim.y - 1 - blockIdx.y) / gridDim.y) * ((n_blocks + DEPTH - 1) / DEPTH);
       uint32_t g = 0, j = blockIdx.y, b = 0;
       for (uint32_t t = 0; t < total + AHEAD; ++t) {
-        if (t >= AHEAD) bar_wait_on(&S.sums_empty[buf.at], buf.round ^ 1u, S);
+        if (t >= AHEAD && !bar_wait_on(&S.sums_empty[buf.at], buf.round ^ 1u, S)) failed = true;
         if (t < total) {
           const uint32_t count = min(SLABS, n_live - g), r0 = (j * BLOCKS + rank) * ROWS;
           for (uint32_t k = b; k < min(b + DEPTH, n_blocks); ++k) {
@@ -577,7 +579,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
         if (t >= AHEAD) {
           asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
           __syncwarp();
-          if (lane == 0) bar_arrive(&S.sums_full[buf.at]);
+          if (lane == 0 && !failed) bar_arrive(&S.sums_full[buf.at]);
           buf.next();
         }
       }
@@ -627,7 +629,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
         const uint32_t lanes = S.tmem + (quarter * 32u << 16) + half * COLS;
         auto read = [&](uint32_t r) { tmem_read<CHUNK>(lanes + buf.at * BUF + r * CHUNK / COLS * Shape::columns + r * CHUNK % COLS, d[r % 2]); };
         auto stage_ready = [&] {
-          bar_wait_on(&S.sums_full[buf.at], buf.round, S);
+          if (!bar_wait_on(&S.sums_full[buf.at], buf.round, S)) failed = true;
           after_sync();
         };
         stage_ready();
@@ -666,7 +668,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
             if (r + 2 == READS) {
               before_sync();
               __syncwarp();
-              if (lane == 0) {
+              if (lane == 0 && !failed) {
                 if (FORM == PAIR) bar_arrive_at<FORM>(at_first<FORM>(&S.both_empty[buf.at]));
                 bar_arrive(&S.sums_empty[buf.at]);
               }
@@ -936,6 +938,11 @@ extern "C" fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_s
   if (cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) return launch_result(e);
   const HeadOperands O{hidden_dev, weight_dev, hidden_stride, weight_stride};
   const HeadArgs A{hidden_scales_dev, hidden_scale_stride, weight_scales_dev, weight_scale_stride, rows, V, K, mask_dev, mask_stride_words,
-                   logits_dev, row_stride_elems};
+                   logits_dev, row_stride_elems, wait_polls.load(std::memory_order_relaxed)};
   return dtype == FMT_BF16 ? head<uint16_t>(O, A, dev, (uint32_t)sms, (cudaStream_t)stream) : head<float>(O, A, dev, (uint32_t)sms, (cudaStream_t)stream);
+}
+
+extern "C" fmt_status fmt_head_set_wait_limit(uint32_t polls) {
+  wait_polls.store(std::min(polls, WAIT_POLLS), std::memory_order_relaxed);
+  return FMT_OK;
 }

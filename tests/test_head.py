@@ -314,6 +314,49 @@ def test_the_same_call_gives_the_same_bits():
             assert torch.equal(first, h.call())
 
 
+@gpu
+@pytest.mark.parametrize("mask", ["none", "mixed", "few"])
+@pytest.mark.parametrize("n", [8, 20, 40, 100, 300])
+def test_waits_that_run_out(n, mask):
+    """With a limit of few polls, waits run out although nothing is wrong, at other places each time (copies on another stream slow the
+    loads down): what comes back is right, or NaN where a token is allowed, and the next call is exact."""
+    torch = torch_()
+    h = Head(n, 30011, 1000, mask, "bf16" if n % 40 else "fp32", seed=n, row_pad=n % 3)
+    right = h.call().clone()
+    h.check()
+    allow = h.allow if h.mask is not None else torch.ones_like(h.allow)
+    block, other = torch.zeros(1 << 28, dtype=torch.uint8, device=DEV), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    try:
+        fmt.head_set_wait_limit(0)
+        h.store.fill_(77.0)
+        got = h.call()
+        assert bool((torch.isnan(got) == allow).all()) and bool((got[~allow] == -torch.inf).all())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            h.call(torch.cuda.current_stream().cuda_stream)
+        for polls in (1, 2, 4, 16) * 3:
+            fmt.head_set_wait_limit(polls)
+            h.store.fill_(77.0)
+            with torch.cuda.stream(other):
+                for _ in range(4):
+                    block.copy_(block.roll(1))
+            got = h.call()
+            assert bool(((got == right) | (torch.isnan(got) & allow)).all())
+            torch.cuda.synchronize()
+    finally:
+        fmt.head_set_wait_limit()
+    h.store.fill_(77.0)
+    assert torch.equal(h.call(), right)
+    h.check()
+    graph.replay()  # a captured call keeps the limit that it was captured with
+    assert bool((torch.isnan(h.logits) == allow).all())
+    assert torch.equal(h.call(), right)
+    fmt.head_set_wait_limit(1 << 31)  # no more than there are otherwise
+    assert torch.equal(h.call(), right)
+    fmt.head_set_wait_limit()
+
+
 def test_refusals():
     """Every one of these is turned down on the host, before anything reaches a GPU."""
     P = 1 << 20  # never read
