@@ -837,7 +837,7 @@ struct HeadOperands {
 };
 
 template <typename T, uint32_t ROWS, HeadForm FORM>
-fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, int dev, uint32_t sms, cudaStream_t st) {
+fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, cudaStream_t st) {
   using Shape = HeadShape<ROWS, FORM>;
   constexpr uint32_t BLOCKS = FORM == PAIR ? 2 : 1;
   CUtensorMap wmap, wmap4, xmap;
@@ -850,11 +850,8 @@ fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, int dev, uint32
     return refuse("the operands cannot be described to the copy engine (a stride of 2^40 bytes or more?)");
   }
   auto* k = head_kernel<T, ROWS, FORM>;
-  static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may have its shared memory
-  if (dev >= 64 || !((allowed.load(std::memory_order_relaxed) >> dev) & 1u)) {
-    if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::smem)) return launch_result(e);
-    if (dev < 64) allowed.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
-  }
+  // asked for every time: it belongs to the context, of which a process may have several, or another after a reset (no difference in 6.9 us a call)
+  if (cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::smem)) return launch_result(e);
   // Rows that need several tiles: a party takes all of them for its slabs (the weights come from L2 after the first), unless
   // the slabs divide badly among the parties; then the tiles of rows are dealt out, too.
   const uint32_t slabs = (A.V + SLAB - 1) / SLAB, row_tiles = (A.rows + BLOCKS * ROWS - 1) / (BLOCKS * ROWS), most = std::max(1u, sms / BLOCKS);
@@ -879,12 +876,12 @@ fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, int dev, uint32
 // 64 rows by tiles of 32 118 / 42.2, by one of 64 91.0 / 29.5, with a lane to a row 109 / 33.6; 128 rows by tiles of 64 154 / 48.6, with a
 // lane to a row 117 / 34.9, in pairs 148 / 44.1; 200 rows with a lane to a row 179 / 58.6, in pairs 157 / 49.1.
 template <typename T>
-fmt_status head(const HeadOperands& O, const HeadArgs& A, int dev, uint32_t sms, cudaStream_t st) {
-  if (A.rows <= 16) return launch_head<T, 16, FEW>(O, A, dev, sms, st);
-  if (A.rows <= 32) return launch_head<T, 32, FEW>(O, A, dev, sms, st);
-  if (A.rows <= 64) return launch_head<T, 64, FEW>(O, A, dev, sms, st);
-  if (A.rows <= WIDE_ROWS) return launch_head<T, WIDE_ROWS, WIDE>(O, A, dev, sms, st);
-  return launch_head<T, WIDE_ROWS, PAIR>(O, A, dev, sms, st);
+fmt_status head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, cudaStream_t st) {
+  if (A.rows <= 16) return launch_head<T, 16, FEW>(O, A, sms, st);
+  if (A.rows <= 32) return launch_head<T, 32, FEW>(O, A, sms, st);
+  if (A.rows <= 64) return launch_head<T, 64, FEW>(O, A, sms, st);
+  if (A.rows <= WIDE_ROWS) return launch_head<T, WIDE_ROWS, WIDE>(O, A, sms, st);
+  return launch_head<T, WIDE_ROWS, PAIR>(O, A, sms, st);
 }
 
 }  // namespace
@@ -939,7 +936,7 @@ extern "C" fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_s
   const HeadOperands O{hidden_dev, weight_dev, hidden_stride, weight_stride};
   const HeadArgs A{hidden_scales_dev, hidden_scale_stride, weight_scales_dev, weight_scale_stride, rows, V, K, mask_dev, mask_stride_words,
                    logits_dev, row_stride_elems, wait_polls.load(std::memory_order_relaxed)};
-  return dtype == FMT_BF16 ? head<uint16_t>(O, A, dev, (uint32_t)sms, (cudaStream_t)stream) : head<float>(O, A, dev, (uint32_t)sms, (cudaStream_t)stream);
+  return dtype == FMT_BF16 ? head<uint16_t>(O, A, (uint32_t)sms, (cudaStream_t)stream) : head<float>(O, A, (uint32_t)sms, (cudaStream_t)stream);
 }
 
 extern "C" fmt_status fmt_head_set_wait_limit(uint32_t polls) {

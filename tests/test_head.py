@@ -8,6 +8,10 @@ order and the rounding of the additions inside a matrix instruction are not spec
   |logit - exact| <= (128 + blocks + 4) 2^-23 * sum over blocks of xs ws sum |x w|
 and half a step of the output's type on top.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
@@ -355,6 +359,65 @@ def test_waits_that_run_out(n, mask):
     fmt.head_set_wait_limit(1 << 31)  # no more than there are otherwise
     assert torch.equal(h.call(), right)
     fmt.head_set_wait_limit()
+
+
+OTHER_CONTEXTS = """
+import ctypes as C, sys
+import numpy as np
+import paper_2506_01151_b200 as fmt
+
+D = C.CDLL("libcuda.so.1")
+def cu(name, *a):
+    r = getattr(D, name)(*a)
+    assert r == 0, (name, r)
+vp = C.c_void_p
+D.cuMemAlloc_v2.argtypes = [C.POINTER(vp), C.c_size_t]
+D.cuMemcpyHtoD_v2.argtypes = [vp, vp, C.c_size_t]
+D.cuMemcpyDtoH_v2.argtypes = [vp, vp, C.c_size_t]
+dev, ctx = C.c_int(), vp()
+cu("cuInit", 0)
+cu("cuDeviceGet", C.byref(dev), 0)
+
+def to_device(a):
+    p = vp()
+    cu("cuMemAlloc_v2", C.byref(p), a.nbytes)
+    cu("cuMemcpyHtoD_v2", p, a.ctypes.data, a.nbytes)
+    return p.value
+
+def logits(n, V=300, K=256):  # of ones: e4m3 1.0 is 0x38
+    y = to_device(np.zeros((n, V), np.float32))
+    fmt.head_logits(to_device(np.full((n, K), 0x38, np.uint8)), to_device(np.ones((2, n), np.float32)), to_device(np.full((V, K), 0x38, np.uint8)),
+                    to_device(np.ones((3, 2), np.float32)), y, fmt.FP32, n, V, K)
+    got = np.zeros((n, V), np.float32)
+    cu("cuCtxSynchronize")
+    cu("cuMemcpyDtoH_v2", got.ctypes.data, y, got.nbytes)
+    assert (got == K).all(), got
+
+def all_forms():
+    for n in (1, 20, 40, 70, 130):
+        logits(n)
+
+if sys.argv[1] == "second":
+    for _ in range(2):
+        cu("cuCtxCreate_v2", C.byref(ctx), 0, dev)
+        all_forms()
+else:
+    for _ in range(2):
+        cu("cuDevicePrimaryCtxRetain", C.byref(ctx), dev)
+        cu("cuCtxSetCurrent", ctx)
+        all_forms()
+        cu("cuDevicePrimaryCtxReset_v2", dev)
+print("both answered")
+"""
+
+
+@gpu
+@pytest.mark.parametrize("how", ["second", "reset"])
+def test_another_context_of_the_same_device(how):
+    """What a kernel is allowed to use belongs to a context: a process that makes a second one, or resets its device, calls on."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", OTHER_CONTEXTS, how], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "both answered" in r.stdout, r.stdout + r.stderr
 
 
 def test_refusals():
