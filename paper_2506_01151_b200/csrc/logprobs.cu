@@ -276,28 +276,43 @@ __device__ __forceinline__ void row_turns(const Row<T>& row, uint32_t from, uint
 // (x - m is formed first: of two logits of the type's lowest value it is 0, where a product with either would overflow.)
 // The entropy is ln s - (t / s) ln 2, two parts of one sign.  A NaN or +inf among the allowed logits makes s NaN, and nothing else does.
 
+// (x - m) / T.  x - m may be beyond fp32 where that over T is not, and so may 1 / T be below its normal numbers: from T = 1 on a quarter of
+// all three is taken, which is exact (of ordinary logits: the same bits).  Below 1, what is beyond fp32 stays so.  The pass takes c alone, but
+// for m, where it grows (2,048 rows of 128,256 bf16: 99.1 us, and 98.5 when it took x - m there).
+constexpr float LOG2E = 1.44269504f;
+struct Heat {
+  float part, c, c_part;  // 1/4 or 1, log2(e) / T, and that over part
+  __device__ __forceinline__ explicit Heat(float temperature) {
+    part = temperature >= 1.0f ? 0.25f : 1.0f;
+    c_part = inv(temperature) * LOG2E, c = part * c_part;
+  }
+  __device__ __forceinline__ float inv(float temperature) const { return __fdiv_rn(1.0f, part * temperature); }  // 1 / T over part
+  __device__ __forceinline__ float apart(float x, float m) const { return __fsub_rn(part * x, part * m); }
+  __device__ __forceinline__ float exponent(float x, float m) const { return apart(x, m) * c_part; }  // (x - m) log2(e) / T
+};
+
 struct Sums {
   float m = -INF, s = 0.0f, t = 0.0f;
 
-  __device__ __forceinline__ void grow(float to, float c) {  // a larger m
+  __device__ __forceinline__ void grow(float to, const Heat& heat) {  // a larger m
     if (!(to > m)) return;
     if (m > -INF) {
-      const float d = (m - to) * c, f = ex2(d);
+      const float d = heat.exponent(m, to), f = ex2(d);
       t = f > 0.0f ? (t + s * d) * f : s * 0.0f;  // (s * 0: what is NaN stays NaN)
       s *= f;
     }
     m = to;
   }
   __device__ __forceinline__ float base() const { return m > -INF ? m : 0.0f; }
-  __device__ __forceinline__ void add(float x, float base, float c) {
-    const float d = (x - base) * c, p = ex2(d);
+  __device__ __forceinline__ void add(float x, float base, const Heat& heat) {
+    const float d = heat.exponent(x, base), p = ex2(d);
     s += p;
     t = fmaf(p, fmaxf(d, -1024.0f), t);  // (d may be -inf; p is 0 below -1024)
   }
   // Units whose largest logits m has grown for.
   template <typename T, uint32_t N>
-  __device__ __forceinline__ void add(const Unit (&x)[N], float c) {
-    const float b = base();
+  __device__ __forceinline__ void add(const Unit (&x)[N], const Heat& heat) {
+    const float b = base(), c = heat.c;
     if (ordinary(m, c)) {
       const uint64_t b2 = two(-b, -b), c2 = two(c, c);
       uint64_t s2 = two(s, 0.0f), t2 = two(t, 0.0f);
@@ -314,15 +329,15 @@ struct Sums {
 #pragma unroll
       for (uint32_t u = 0; u < N; ++u)
 #pragma unroll
-        for (uint32_t e = 0; e < 32u / sizeof(T); ++e) add(value(x[u], e, T()), b, c);
+        for (uint32_t e = 0; e < 32u / sizeof(T); ++e) add(value(x[u], e, T()), b, heat);
     }
   }
   template <uint32_t LANES>
-  __device__ __forceinline__ void join_lanes(float c) {  // of a warp's first so many lanes, all of which get the result
+  __device__ __forceinline__ void join_lanes(const Heat& heat) {  // of a warp's first so many lanes, all of which get the result
     float most = m;
 #pragma unroll
     for (uint32_t o = LANES / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-    grow(most, c);
+    grow(most, heat);
 #pragma unroll
     for (uint32_t o = LANES / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o), t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
   }
@@ -542,8 +557,7 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
   before_me();
   const uint32_t rank = cluster > 1 ? cluster_rank() : 0u, row_id = blockIdx.x / cluster;
   const Row<T> row(R, row_id);
-  const float temperature = R.temperature ? R.temperature[row_id] : 1.0f;
-  const float inv = __fdiv_rn(1.0f, temperature), c = inv * 1.44269504f;  // log2(e)
+  const Heat heat(R.temperature ? R.temperature[row_id] : 1.0f);
   int32_t token = -1;  // (asked for now, wanted at the end)
   float token_logit = 0.0f;
   if (rank == 0 && tid < R.n_tokens) {
@@ -557,7 +571,7 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
   if (tid < edges && row.edge(tid) < row.head) {
     const float x = row.at(row.edge(tid));
     if (x > a.m) where = row.units + tid;
-    a.grow(x, c), a.add(x, a.base(), c);
+    a.grow(x, heat), a.add(x, a.base(), heat);
   }
 
   const uint32_t from = rank * THREADS + tid, step = cluster * THREADS;
@@ -565,14 +579,14 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
     const float most = largest(x, T());
     if (most > a.m) {
       if (TOP) where = i;
-      a.grow(most, c);
+      a.grow(most, heat);
     }
-    a.template add<T, UNROLL>(x, c);
+    a.template add<T, UNROLL>(x, heat);
   });
   if (tid < edges && row.edge(tid) >= row.head) {
     const float x = row.at(row.edge(tid));
     if (x > a.m) where = row.units + tid;
-    a.grow(x, c), a.add(x, a.base(), c);
+    a.grow(x, heat), a.add(x, a.base(), heat);
   }
 
   if (TOP) {
@@ -597,12 +611,13 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
     find_top<T, MASK>(row, keep, from, step, edges, mine, O.n_top, P);
   }
 
-  a.join_lanes<32>(c);
+  const float temperature = R.temperature ? *const_cast<const volatile float*>(R.temperature + row_id) : 1.0f;  // (not kept in the pass)
+  a.join_lanes<32>(heat);
   if (tid % 32u == 0) J.warps[tid / 32u] = a;
   __syncthreads();
   if (tid < 32) {
     a = tid < WARPS ? J.warps[tid] : Sums();
-    a.join_lanes<WARPS>(c);
+    a.join_lanes<WARPS>(heat);
   }
   if (cluster > 1) {
     cluster_wait();  // the first block has begun: its memory may be written
@@ -616,7 +631,7 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
     if (rank) return;
     if (tid < 32) {
       a = tid < cluster ? J.blocks[tid] : Sums();
-      a.join_lanes<MAX_CLUSTER>(c);
+      a.join_lanes<MAX_CLUSTER>(heat);
     }
     if (TOP) {
       // the blocks' lists are in order: a key's place is its own in its list and, of every other one, how many are above
@@ -646,7 +661,8 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
   const float nan = __int_as_float(0x7FC00000);
   const bool bad = a.s != a.s || !(temperature >= 0x1p-126f && temperature < INF);  // (below, log2(e) / T overflows)
   const float ln = bad ? nan : logf(a.s);  // (-inf of nothing)
-  auto logprob = [&](float x) { return bad ? nan : x == -INF ? -INF : (x - a.m) * inv - ln; };
+  const float inv = heat.inv(temperature);
+  auto logprob = [&](float x) { return bad ? nan : x == -INF ? -INF : heat.apart(x, a.m) * inv - ln; };
   const bool wrong = token < -1 || token >= (int64_t)R.V;
   if (tid < R.n_tokens && O.logprobs) O.logprobs[(size_t)row_id * R.n_tokens + tid] = token == -1 ? 0.0f : wrong ? nan : logprob(token_logit);
   if (TOP && tid < O.n_top) {
@@ -670,7 +686,7 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
 // grad = (p (A + B lp2) + the g of the given tokens) / T with lp2 = log2 p, A = -(sum g + g_H H) and B = -g_H ln 2.  In ordinary rows 1 / T is
 // part of A, B and g; in others, where that may be beyond fp32 (1 / T is up to 2^126, and so may the incoming gradients be), it comes last, and
 // what p = 0 is multiplied with is not looked at.  A row's sizes decide, not a logit's, and the loop costs nothing for it (2,048 rows of 128,256
-// bf16: 166 us, 168 before; 48 rows of 50,001 fp32 with three given tokens 7.2, 7.1 before).
+// bf16: 166 us, 168 before; 48 rows of 50,001 fp32 with three given tokens 7.3, 7.1 before).
 // The given tokens' own logits decide whether they count: all of a cluster's blocks have read them before the first writes,
 // since the gradient may take the logits' place.
 
@@ -684,13 +700,15 @@ __global__ void __launch_bounds__(THREADS, 4) logprobs_backward_kernel(const Row
   before_me();
   const uint32_t rank = cluster > 1 ? cluster_rank() : 0u, row_id = blockIdx.x / cluster;
   const Row<T> row(R, row_id);
-  const float inv = __fdiv_rn(1.0f, R.temperature ? R.temperature[row_id] : 1.0f), c = inv * 1.44269504f;
-  const float most = D.norm[2 * (size_t)row_id], ln = D.norm[2 * (size_t)row_id + 1], log2s = ln * 1.44269504f;
+  const float temperature = R.temperature ? R.temperature[row_id] : 1.0f;
+  const Heat heat(temperature);
+  const float inv_part = heat.inv(temperature), inv = heat.part * inv_part, c = heat.c;
+  const float most = D.norm[2 * (size_t)row_id], ln = D.norm[2 * (size_t)row_id + 1], log2s = ln * LOG2E;
   const float gh = D.by_entropy ? D.by_entropy[row_id] : 0.0f, h = D.by_entropy ? D.entropy[row_id] : 0.0f;
   const uint32_t n_tokens = D.by_logprob ? R.n_tokens : 0u;
   if (tid < n_tokens) {
     const int32_t v = R.tokens[(size_t)row_id * R.n_tokens + tid];
-    const bool ok = v >= 0 && v < (int64_t)R.V && (row.at((uint32_t)v) - most) * inv > -INF;
+    const bool ok = v >= 0 && v < (int64_t)R.V && heat.apart(row.at((uint32_t)v), most) * inv_part > -INF;
     tok[tid] = ok ? v : -1;
     g[tid] = ok ? D.by_logprob[(size_t)row_id * R.n_tokens + tid] : 0.0f;
   }
@@ -703,11 +721,11 @@ __global__ void __launch_bounds__(THREADS, 4) logprobs_backward_kernel(const Row
   const bool aligned = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.x)) & 31u) == 0;
   auto grad = [&](float x, uint32_t v) {
     if (x == -INF) return 0.0f;
-    const float lp2 = fmaf(x - most, c, -log2s), p = exp2f(lp2);
+    const float lp2 = fmaf(heat.apart(x, most), heat.c_part, -log2s), p = exp2f(lp2);
     float d = p == 0.0f ? 0.0f : p * fmaf(B, lp2, A);
     for (uint32_t k = 0; k < n_tokens; ++k)
       if (tok[k] == (int32_t)v) d += g[k];
-    return d * inv;
+    return heat.part * d * inv_part;
   };
   if (rank == 0 && tid < row.edges) {
     const uint32_t v = row.edge(tid);

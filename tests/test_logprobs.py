@@ -352,6 +352,23 @@ def test_gradients_that_are_not_finite_reach_allowed_tokens_only(by, value, dtyp
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("temperature", [1.0, 3.0, 1e8, 1e30, 1e37, 2e38, 3.4e38])
+def test_logits_farther_apart_than_the_largest_number(temperature, dtype):
+    """x - M may be beyond fp32 where (x - M) / T is not."""
+    torch = torch_()
+    i = Inputs(5, 4099, dtype, "mixed", offset=1, n_tokens=4, seed=13, scale=1.0)
+    i.logits.copy_((i.logits.float().clamp(-3.3, 3.3) * 1e38).to(i.type))
+    i.allow[:, :4] = True
+    i.logits[:, 0], i.logits[:, 1] = torch.finfo(i.type).max, torch.finfo(i.type).min
+    i.tokens[:, 0], i.tokens[:, 1] = 0, 1
+    i.temperature[:] = temperature
+    out = i.forward()
+    check_forward(i, out)
+    check_gradient_of_any_size(i, out)
+
+
+@gpu
 @pytest.mark.parametrize("n_tokens", [0, 1, 32])
 @pytest.mark.parametrize("with_g,with_h", [(True, False), (False, True), (False, False)])
 def test_gradients_that_are_not_given(n_tokens, with_g, with_h):
