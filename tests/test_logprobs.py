@@ -369,6 +369,32 @@ def test_logits_farther_apart_than_the_largest_number(temperature, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("mask", ["none", "all"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_long_rows_of_equal_logits(dtype, mask):
+    """As many equal logits as a server's largest batch leaves to one thread block, behind a few that are larger, some for each thread: the
+    terms of a thread are all the same then, and a chain of additions would round each of them the same way.  A thread adds up 32 terms
+    (17 roundings at most, by pairs), and then those sums, V / 8,192 of them (fp32: half as many terms, twice as many sums); 13 more roundings
+    join the threads of a block.  The terms themselves are off by 4 |d| + 4 units (what d takes, and exp), the logarithm by two of its own."""
+    torch = torch_()
+    V, n, large = 1 << 18, 320, 1024
+    i = Inputs(n, V, dtype, mask, heat=False, n_tokens=1, seed=14)
+    at = -0.25 - torch.arange(n, device=DEV, dtype=torch.float32) / 128  # (what bf16 makes of it is the input)
+    i.logits[:] = at.to(i.type)[:, None]
+    i.logits[:, : 8 * large : 8] = 0.0
+    norm, entropy = torch.zeros((n, 2), device=DEV), torch.zeros(n, device=DEV)
+    fmt.token_logprobs(i.logits, i.dtype, n, V, norm_dev=norm, entropy_dev=entropy, mask_dev=i.mask())
+    d = i.logits[:, 1].double()
+    S = large + (V - large) * torch.exp(d)
+    H = torch.log(S) - (V - large) * d * torch.exp(d) / S
+    unit = U * (17 + V / (8192 if dtype == "bf16" else 4096) + 13 + 4 * d.abs() + 4)  # relative, of S and of the sum of p d
+    err, limit = (norm[:, 1].double() - torch.log(S)).abs(), unit + 2 * U * torch.log(S)
+    assert bool((err <= limit).all()), float((err / limit).max())
+    err, limit = (entropy.double() - H).abs(), (2 * unit + 4 * U) * (2 + H)
+    assert bool((err <= limit).all()), float((err / limit).max())
+
+
+@gpu
 @pytest.mark.parametrize("n_tokens", [0, 1, 32])
 @pytest.mark.parametrize("with_g,with_h", [(True, False), (False, True), (False, False)])
 def test_gradients_that_are_not_given(n_tokens, with_g, with_h):
