@@ -930,13 +930,12 @@ extern "C" fmt_status fmt_head_logits(const uint8_t* hidden_dev, size_t hidden_s
     return refuse("a pointer is not aligned to its elements");
   if (rows == 0) return FMT_OK;
   if (fmt_status s = reachable({hidden_dev, hidden_scales_dev, weight_dev, weight_scales_dev, mask_dev, logits_dev})) return s;
-  int dev = 0, sms = 0;
-  if (cudaError_t e = cudaGetDevice(&dev)) return launch_result(e);
-  if (cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev)) return launch_result(e);
+  uint32_t sms;
+  if (fmt_status s = count_sms(&sms)) return s;
   const HeadOperands O{hidden_dev, weight_dev, hidden_stride, weight_stride};
   const HeadArgs A{hidden_scales_dev, hidden_scale_stride, weight_scales_dev, weight_scale_stride, rows, V, K, mask_dev, mask_stride_words,
                    logits_dev, row_stride_elems, wait_polls.load(std::memory_order_relaxed)};
-  return dtype == FMT_BF16 ? head<uint16_t>(O, A, (uint32_t)sms, (cudaStream_t)stream) : head<float>(O, A, (uint32_t)sms, (cudaStream_t)stream);
+  return dtype == FMT_BF16 ? head<uint16_t>(O, A, sms, (cudaStream_t)stream) : head<float>(O, A, sms, (cudaStream_t)stream);
 }
 
 extern "C" fmt_status fmt_head_set_wait_limit(uint32_t polls) {

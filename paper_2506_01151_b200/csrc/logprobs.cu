@@ -369,9 +369,10 @@ __device__ __forceinline__ uint64_t max_key(uint64_t a, uint64_t b) { return a >
 // the n_top groups whose own largest reaches it hold any: their units alone are read again (L2), and what reaches the bound is
 // listed and put in order.  A row of 128,256 logits is passed once, and a sixth of it twice for n_top = 20, whatever its order.
 
-constexpr uint32_t THREADS = 256, WARPS = THREADS / 32, UNROLL = 2, BACK_UNROLL = 1;
-// Blocks to an SM: four have 64 registers a thread, which a masked pass outgrows (2,048 rows of 128,256 bf16, four and three: masked 124 and
-// 109 us, unmasked 98.5 and 101).
+constexpr uint32_t THREADS = 256, WARPS = THREADS / 32, UNROLL = 2, BACK_UNROLL = 1, BACK_PER_SM = 4;
+// Blocks to an SM: four have 64 registers a thread, which a masked pass outgrows (masked rows of 128,256 bf16, us with three and with four, without
+// and with 20 alternatives: 48 rows 5.9 and 7.0, 12.4 and 14.1; 256 rows, where four run two blocks to a row at a time, 21.4 and 17.7, 30.2
+// and 28.8; 2,048 rows 87.6 and 88.6, 129 and 147; 1,024 rows of fp32 75 and 71, 108 and 104.  Unmasked, 2,048 rows: 101 and 98.5).
 constexpr uint32_t per_sm(bool masked) { return masked ? 3u : 4u; }
 constexpr uint32_t GROUPS = 128, GROUP = THREADS / GROUPS;
 constexpr uint32_t MAX_CLUSTER = 8;
@@ -696,7 +697,7 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
 // since the gradient may take the logits' place.
 
 template <typename T, bool MASK>
-__global__ void __launch_bounds__(THREADS, 4) logprobs_backward_kernel(const Rows R, const Gradients D, const uint32_t cluster) {
+__global__ void __launch_bounds__(THREADS, BACK_PER_SM) logprobs_backward_kernel(const Rows R, const Gradients D, const uint32_t cluster) {
   __shared__ int32_t tok[FMT_MAX_GIVEN_TOKENS];
   __shared__ float g[FMT_MAX_GIVEN_TOKENS];
   __shared__ Keep<T> keep;
@@ -785,13 +786,15 @@ __global__ void __launch_bounds__(THREADS, 4) logprobs_backward_kernel(const Row
   });
 }
 
-// Blocks to a row: as many as run at a time (`resident` to an SM), while each has a unit for every thread at least.  A block that
-// looks for alternatives spends several microseconds on them however short its part is, so of those there are two to an SM (rows of
-// 50,001 with 5 alternatives, 48 of them: 8 blocks a row 14.3 us, 4 12.2, 2 12.1; 64 rows of 128,256 with 20: 18.4, 15.1, 17.0).  The
-// second block is worth it even so (256 masked rows of 128,256 with 20 alternatives: one 39.2, two 30.9, four 38.7; without: 31, 20).
-uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width, uint32_t resident, bool top) {
+// Blocks to a row: as many as run at a time (`resident` to an SM), while each has a unit for every thread at least.  A second wave of
+// blocks costs more than halves of rows save: 256 masked rows of 128,256 bf16 with 20 alternatives take 33.6 us from memory with a block
+// each and 43.1 with two, without alternatives 24.8 and 29.5; 222 rows, whose two blocks all run at a time, 32.1 and 28.9, 24.0 and 21.2.
+// A block that looks for alternatives spends several microseconds on them however short its part is, so of those there are no more
+// than two to an SM from the third block to a row on (rows of 50,001 with 5 alternatives, 48 of them: 8 blocks a row 14.3 us, 4 12.2,
+// 2 12.1; 64 rows of 128,256 with 20: 18.4, 15.1, 17.0).
+uint32_t cluster_size(uint32_t rows, uint32_t V, uint32_t width, uint32_t resident, bool top, uint32_t sms) {
   uint32_t c = 1;
-  while (c < MAX_CLUSTER && rows * (c * 2u) <= (c == 1 ? 4u : top ? 2u : resident) * 148u && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
+  while (c < MAX_CLUSTER && (uint64_t)rows * c * 2u <= (uint64_t)(top && c > 1 ? 2u : resident) * sms && (uint64_t)c * 2u * THREADS * width <= V) c *= 2u;
   return c;
 }
 
@@ -839,7 +842,9 @@ extern "C" fmt_status fmt_token_logprobs(const void* logits_dev, fmt_dtype dtype
                                 top_ids_dev, top_logprobs_dev, status_dev}))
     return s;
   const Outputs O{top_ids_dev || top_logprobs_dev ? n_top : 0u, logprobs_dev, norm_dev, entropy_dev, top_ids_dev, top_logprobs_dev, status_dev};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, per_sm(mask_dev != nullptr), O.n_top != 0);
+  uint32_t sms;
+  if (fmt_status s = count_sms(&sms)) return s;
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, per_sm(mask_dev != nullptr), O.n_top != 0, sms);
   void (*k)(Rows, Outputs, uint32_t);
   if (dtype == FMT_BF16)
     k = mask_dev ? O.n_top ? logprobs_kernel<uint16_t, true, true> : logprobs_kernel<uint16_t, true, false>
@@ -869,7 +874,9 @@ extern "C" fmt_status fmt_token_logprobs_backward(const void* logits_dev, fmt_dt
                                 grad_entropy_dev, grad_logits_dev}))
     return s;
   const Gradients D{norm_dev, entropy_dev, grad_logprobs_dev, grad_entropy_dev, grad_logits_dev, grad_stride_elems};
-  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, 4, false);
+  uint32_t sms;
+  if (fmt_status s = count_sms(&sms)) return s;
+  const uint32_t cluster = cluster_size(rows, V, dtype == FMT_BF16 ? 16 : 8, BACK_PER_SM, false, sms);
   auto* k = dtype == FMT_BF16 ? mask_dev ? logprobs_backward_kernel<uint16_t, true> : logprobs_backward_kernel<uint16_t, false>
                               : mask_dev ? logprobs_backward_kernel<float, true> : logprobs_backward_kernel<float, false>;
   return launch_result(launch_clusters(k, rows, cluster, (cudaStream_t)stream, R, D, cluster));

@@ -41,4 +41,12 @@ inline fmt_status reachable(std::initializer_list<const void*> ptrs) {
   return FMT_OK;
 }
 
+inline fmt_status count_sms(uint32_t* sms) {  // of the current device
+  int dev = -1, n = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return launch_result(e);
+  if (cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev)) return launch_result(e);
+  *sms = (uint32_t)n;
+  return FMT_OK;
+}
+
 }  // namespace fmt
