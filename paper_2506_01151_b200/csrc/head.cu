@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
   auto slab_no = [&](uint32_t i) { return place(i, fours); };
   // Small masks are looked at as a whole by every block, and what is left of the vocabulary is dealt out anew: where a grammar leaves
   // few tokens, a block's own slabs have five or six of them, or none (8 rows of 32,000 x 4,096: 19.2 us, so 13.4).
-  const bool whole = A.mask && n_slabs <= ALL_SLABS && (uint64_t)n_slabs * A.rows <= ALL_WORDS && n_slabs > parties && n_mine < LIST;
+  const bool whole = A.mask && n_slabs <= ALL_SLABS && (uint64_t)n_slabs * A.rows <= ALL_WORDS && n_slabs > parties;  // (a block has no more of those than of all)
   // The block's slabs that some row may use, and the others.
   if (whole) {
     // lanes are slabs, whose words lie side by side; four times 32 slabs and eight rows are asked for at a time
