@@ -489,6 +489,58 @@ def test_memory_that_the_device_cannot_reach_is_refused():
 
 
 @gpu
+def test_steps_back_to_back_on_two_streams():
+    """Hidden states -> 8-bit blocks -> masked logits -> log probabilities -> gradient in the logits' place, many steps without a pause on two
+    streams at a time (launches overlap: a kernel begins while the one before is still running), against one call after the other."""
+    torch = torch_()
+    steps, K = 12, 700
+    cases = []
+    for n, V, mask in ((9, 20011, "few"), (200, 6000, "mixed")):
+        h = Head(n, V, K, mask, "bf16", seed=n)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(n)
+        hidden = torch.randn((steps, n, K), generator=g, device=DEV).to(torch.bfloat16)
+        cases.append((h, hidden, torch.randint(0, V, (n, 2), generator=g, device=DEV, dtype=torch.int32), torch.randn((n, 2), generator=g, device=DEV),
+                      torch.randn(n, generator=g, device=DEV)))
+
+    def outputs():
+        f = dict(dtype=torch.float32, device=DEV)
+        return [dict(q=torch.zeros((n, h.hs), dtype=torch.uint8, device=DEV), s=torch.zeros((up(K, 128), n), **f),
+                     y=torch.zeros((steps, n, h.V), dtype=torch.bfloat16, device=DEV), lp=torch.zeros((steps, n, 2), **f), norm=torch.zeros((steps, n, 2), **f),
+                     H=torch.zeros((steps, n), **f), ids=torch.zeros((steps, n, 3), dtype=torch.int32, device=DEV)) for h, *_ in cases for n in [h.n]]
+
+    def step(i, case, o, stream, pause):
+        h, hidden, tokens, g, gh = case
+        fmt.quantize_blocks(hidden[i], fmt.BF16, h.n, K, 1, o["q"], o["s"], q_stride=h.hs, stream=stream)
+        pause()
+        fmt.head_logits(o["q"], o["s"], h.w, h.wscale, o["y"][i], fmt.BF16, h.n, h.V, K, mask_dev=h.mask, hidden_stride=h.hs, weight_stride=h.ws,
+                        weight_scale_stride=h.wss, stride_words=h.mask_stride, stream=stream)
+        pause()
+        fmt.token_logprobs(o["y"][i], fmt.BF16, h.n, h.V, tokens_dev=tokens, n_tokens=2, logprobs_dev=o["lp"][i], norm_dev=o["norm"][i], entropy_dev=o["H"][i],
+                           n_top=3, top_ids_dev=o["ids"][i], mask_dev=h.mask, stride_words=h.mask_stride, stream=stream)
+        pause()
+        fmt.token_logprobs_backward(o["y"][i], fmt.BF16, h.n, h.V, o["norm"][i], o["y"][i], tokens_dev=tokens, n_tokens=2, grad_logprobs_dev=g,
+                                    entropy_dev=o["H"][i], grad_entropy_dev=gh, mask_dev=h.mask, stride_words=h.mask_stride, stream=stream)
+        pause()
+
+    want = outputs()
+    for case, o in zip(cases, want):
+        for i in range(steps):
+            step(i, case, o, 0, torch.cuda.synchronize)
+    assert all(len(torch.unique(o["ids"][:, 0, 0])) > 1 for o in want)  # the steps are not alike
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(3):
+        got = outputs()
+        torch.cuda.synchronize()
+        for i in range(steps):
+            for case, o, s in zip(cases, got, streams):
+                step(i, case, o, s.cuda_stream, lambda: None)
+        torch.cuda.synchronize()
+        for o, w in zip(got, want):
+            assert all(torch.equal(o[k].view(torch.uint8), w[k].view(torch.uint8)) for k in w)
+
+
+@gpu
 def test_a_decoding_loop_from_hidden_states_to_the_next_token():
     """Masks from the grammar, logits from the 8-bit head under them, the likeliest token back into the state: every token
     taken is one that the oracle allows, and the distribution is that of the masked logits."""
