@@ -422,6 +422,7 @@ fmt_status fmt_fill_mask_noalloc(const fmt_grammar* g, const uint32_t* charts_de
  *                128: weights, a scale for each 128 x 128: scales_dev[(row / 128) * scale_stride + block],
  *                   scale_stride >= ceil(cols / 128)
  *   q_dev        bytes, rows q_stride bytes apart; bytes beyond `cols` are left as they were
+ * cols at most 2^20, rows at most 2^24, and together fewer than 2^31 thread blocks (of 8 x 128 values, or of 128 x 128).
  */
 fmt_status fmt_quantize_blocks(const void* x_dev, fmt_dtype dtype, uint32_t rows, uint32_t cols, size_t row_stride_elems,
                                uint32_t block_rows, uint8_t* q_dev, size_t q_stride, float* scales_dev, size_t scale_stride,
@@ -431,7 +432,8 @@ fmt_status fmt_quantize_blocks(const void* x_dev, fmt_dtype dtype, uint32_t rows
  * The output head: logits of every row under its mask.
  *   logits[i][v] = sum over blocks b of 128 columns: hidden_scales[b][i] * weight_scales[v / 128][b]
  *                                                    * sum over k in block b: hidden[i][k] * weight[v][k]
- * with e4m3 values and sums in fp32, rounded once to `dtype`; -inf (as fmt_apply_mask writes it) where bit v of row i's mask
+ * with e4m3 values and sums in fp32 (the two scales are multiplied with one another first: what their product loses of a denormal,
+ * or beyond fp32, is lost), rounded once to `dtype`; -inf (as fmt_apply_mask writes it) where bit v of row i's mask
  * is 0.  Weights of 32 tokens in a row (a mask word) that no row may use are not read.
  *   hidden_dev   [rows][K] e4m3 bytes and hidden_scales_dev, as fmt_quantize_blocks writes them with block_rows = 1
  *   weight_dev   [V][K] e4m3 bytes and weight_scales_dev, as it writes them with block_rows = 128
@@ -465,9 +467,11 @@ fmt_status fmt_head_set_wait_limit(uint32_t polls);
  *                     -1 where fewer are allowed.  With n_top = 1 these are the greedy tokens, as fmt_state_advance takes them
  *   top_logprobs_dev  [rows][n_top] their ln p, -inf beside -1
  *   status_dev        [rows] int32: FMT_OK, or FMT_ERR_INVALID_ARG: a given token is not in [-1, V) (its log probability is NaN,
- *                     the others stand), or the temperature is not a positive normal number (2^-126 or more, finite), or an allowed logit is NaN or
- *                     +inf (all the row's outputs are NaN, its alternatives -1)
+ *                     the others stand), or the temperature is not a positive normal number (2^-126 or more, finite), or an
+ *                     allowed logit is NaN or +inf (the row's outputs are NaN, its alternatives -1; beside a given token of -1
+ *                     stands 0 as ever)
  * A row without an allowed token: log probabilities -inf, M and ln S -inf, entropy 0, alternatives -1.
+ * V at most 2^30, rows at most 2^24; the same holds for the gradient.
  */
 #define FMT_MAX_GIVEN_TOKENS 32
 #define FMT_MAX_TOP 32
