@@ -460,6 +460,57 @@ def test_rows_farther_apart_than_32_bits(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("masked", [False, True])
+def test_the_longest_rows(masked):
+    """A row of 2^30 bf16 logits, all alike but for a few: sums, ids and gradients at both ends and in the middle.  A thread of the 2,048
+    adds up 2^14 sums of 32 terms: 2^14 + 33 roundings, and 4 |d| + 4 for the terms."""
+    torch = torch_()
+    V, low, places = 1 << 30, -8.0, [3, 17, (1 << 29) + 5, (1 << 30) - 2]
+    values = [9.0, 10.0, 9.5, 8.5]
+    x = torch.full((V,), low, dtype=torch.bfloat16, device=DEV)
+    x[places] = torch.tensor(values, dtype=torch.bfloat16, device=DEV)
+    mask = torch.full((V // 32,), -1, dtype=torch.int32, device=DEV) if masked else None
+    if masked:
+        mask[1 << 20: 1 << 24] = 0
+    tokens = torch.tensor([places + [V - 1, 1 << 25]], dtype=torch.int32, device=DEV)
+    lp, norm, H = torch.zeros((1, 6), device=DEV), torch.zeros((1, 2), device=DEV), torch.zeros(1, device=DEV)
+    ids, status = torch.zeros((1, 6), dtype=torch.int32, device=DEV), torch.full((1,), 77, dtype=torch.int32, device=DEV)
+    kw = dict(tokens_dev=tokens, n_tokens=6, mask_dev=mask)
+    fmt.token_logprobs(x, fmt.BF16, 1, V, logprobs_dev=lp, norm_dev=norm, entropy_dev=H, n_top=6, top_ids_dev=ids, status_dev=status, **kw)
+    others = V - 4 - (((1 << 24) - (1 << 20)) * 32 if masked else 0)
+    d = np.array(values + [low]) - 10.0
+    many = np.array([1, 1, 1, 1, others])
+    S = (many * np.exp(d)).sum()
+    ln = d - np.log(S)
+    entropy = -(many * np.exp(ln) * ln).sum()
+    off = U * ((1 << 14) + 33 + 4 * 18 + 4)
+    assert status.item() == 0 and ids[0].tolist() == [17, (1 << 29) + 5, 3, V - 2, 0, 1]
+    assert norm[0, 0].item() == 10.0 and abs(norm[0, 1].item() - np.log(S)) < off + 2 * U * np.log(S)
+    gone = masked and (1 << 20) <= (1 << 25) // 32 < (1 << 24)
+    want = np.array(list(ln) + [-np.inf if gone else ln[4]])
+    got = lp[0].double().cpu().numpy()
+    assert got[5] == want[5] if gone else True
+    assert (np.abs(got[:5] - want[:5]) < off + 8 * U * np.abs(want[:5])).all()
+    assert abs(H.item() - entropy) < (2 * off + 8 * U) * (2 + entropy)
+    g, gh = torch.tensor([[0.5, -1.0, 0.25, 2.0, 1.5, 0.75]], device=DEV), torch.tensor([0.7], device=DEV)
+    fmt.token_logprobs_backward(x, fmt.BF16, 1, V, norm, x, grad_logprobs_dev=g, entropy_dev=H, grad_entropy_dev=gh, **kw)  # in the logits' place
+    gs = g[0].double().cpu().numpy()
+    if gone:
+        gs[5] = 0.0
+    p = np.exp(ln)
+    base = -p * gs.sum() - 0.7 * p * (ln + entropy)
+    grad = x[places + [V - 1, 1 << 25, 0, (1 << 29) - 1]].double().cpu().numpy()
+    more = base[4] if not masked else 0.0
+    wants = np.array([base[0] + gs[0], base[1] + gs[1], base[2] + gs[2], base[3] + gs[3], base[4] + gs[4], 0.0 if gone else base[4] + gs[5], base[4], more])
+    assert (np.abs(grad - wants) <= 2.0 ** -8 * np.abs(wants) + 2 * off * (1 + gs.sum()) * 4).all(), (grad, wants)
+    assert int((x == x[0]).sum()) == others - (1 if gone else 2)  # all that are alike but tokens that were given
+    if masked:
+        assert int((x == 0).sum()) == V - 4 - others
+    del x
+    torch.cuda.empty_cache()
+
+
+@gpu
 def test_captured_replayed_and_on_other_streams():
     """Two graphs of the same call with other inputs, replayed at the same time on two streams, several times."""
     torch = torch_()
