@@ -53,7 +53,10 @@ __device__ __forceinline__ void store4(uint8_t* q, uint32_t n, bool aligned, flo
 }
 
 // Hidden states: a warp to 128 values of a row, four to a lane.  Weights: a thread block to 128 x 128, 16 rows to a warp, which keeps
-// them in registers until the block's largest is known.  Either way a value is read once.
+// them in registers until the block's largest is known.  Either way a value is read once.  Us of bf16 and fp32, and those of the
+// bytes: hidden states 64 x 4,096 1.8, 2,048 x 4,096 12.8 and 12.7 (3.8, 6.4), 8,192 x 8,192 98 and 97 (31, 51), which instructions bound
+// (180 for four values, the quotients in IEEE single precision among them; 85 % of all issue slots); weights 128,256 x 4,096, once a
+// model, 1,313 and 654 (241, 401), with a quarter of the warps, of which bf16 ones wait for their loads most of the time.
 constexpr uint32_t QUANTIZE_WARPS = 8;
 template <typename T, uint32_t ROWS>
 __global__ void __launch_bounds__(QUANTIZE_WARPS * 32) quantize_kernel(const T* x, uint32_t rows, uint32_t cols, size_t row_stride, uint8_t* q,
@@ -114,8 +117,11 @@ constexpr uint32_t SLAB = 32;
 constexpr uint32_t HEAD_THREADS = 384, ADD_WARPS = 8;
 constexpr uint32_t LIST = 512;        // slabs of a block, at most
 constexpr uint32_t MOST_TOKENS = 1u << 20;
-constexpr uint32_t ALL_SLABS = 8192;  // of a vocabulary whose masks every block looks at as a whole
-constexpr uint32_t ALL_WORDS = 32768; // of the masks then
+// Masks that every block looks at as a whole, and of what vocabularies (whose bits are 1 KB then).  Looking takes every block the time of all
+// words: us of 32,000 and of 128,256 x 4,096 with a block's own slabs alone, and as a whole: 8 narrow rows 13.3 and 10.6, 14.2 and 13.2; 16
+// rows 13.8 and 11.9, 15.8 and 16.7; 32 rows 20.4 and 17.5, 36.8 and 36.7; 64 rows 26 and 34, 50 and 70; where half of the rows may use all
+// slabs, nothing is won: 8 rows 24.7 and 26.3, 83.3 and 87.1; 32 rows 25.8 and 30.6, 87 and 102.
+constexpr uint32_t ALL_SLABS = 8192, ALL_WORDS = 32768;
 constexpr uint32_t SCALE_SLOTS = 8;
 constexpr uint32_t SLAB_BYTES = SLAB * BLOCK;
 constexpr uint32_t WAIT_POLLS = 1u << 18;  // of 2,900 cycles, the time after which a wait for nothing comes back
@@ -376,7 +382,7 @@ __global__ void __launch_bounds__(HEAD_THREADS, 1) head_kernel(const __grid_cons
   const uint32_t fours = n_slabs / (4u * parties), n_mine = share(n_slabs, fours);
   auto slab_no = [&](uint32_t i) { return place(i, fours); };
   // Small masks are looked at as a whole by every block, and what is left of the vocabulary is dealt out anew: where a grammar leaves
-  // few tokens, a block's own slabs have five or six of them, or none (8 rows of 32,000 x 4,096: 19.2 us, so 13.4).
+  // few tokens, a block's own slabs have five or six of them, or none (8 rows of 32,000 x 4,096: 13.3 us, so 10.6).
   const bool whole = A.mask && n_slabs <= ALL_SLABS && (uint64_t)n_slabs * A.rows <= ALL_WORDS && n_slabs > parties;  // (a block has no more of those than of all)
   // The block's slabs that some row may use, and the others.
   if (whole) {
@@ -874,7 +880,8 @@ fmt_status launch_head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, c
 
 // us, 128,256 x 4,096 / 32,000 x 4,096: 32 rows by tiles of 16 106 / 45.7, by one of 32 90.4 / 33.8; 16 rows 87.9 / 29.6 and 89.8 / 31.3.
 // 64 rows by tiles of 32 118 / 42.2, by one of 64 91.0 / 29.5, with a lane to a row 109 / 33.6; 128 rows by tiles of 64 154 / 48.6, with a
-// lane to a row 117 / 34.9, in pairs 148 / 44.1; 200 rows with a lane to a row 179 / 58.6, in pairs 157 / 49.1.
+// lane to a row 117 / 34.9, in pairs 148 / 44.1; 200 rows with a lane to a row 179 / 58.6, in pairs 157 / 49.1.  fp32 logits: 128 rows 120 / 37.2
+// (bf16 110 / 33.9 then), 256 rows 170 / 58.0, 1,024 rows 591 / 166.
 template <typename T>
 fmt_status head(const HeadOperands& O, const HeadArgs& A, uint32_t sms, cudaStream_t st) {
   if (A.rows <= 16) return launch_head<T, 16, FEW>(O, A, sms, st);

@@ -367,7 +367,8 @@ __device__ __forceinline__ uint64_t max_key(uint64_t a, uint64_t b) { return a >
 // The likeliest tokens.  In the pass over the row each thread keeps the first units with its largest logit.  The threads make
 // 128 groups; of the groups' largest keys (logit, lowest id) the n_top-th is a bound that n_top logits at least reach, and only
 // the n_top groups whose own largest reaches it hold any: their units alone are read again (L2), and what reaches the bound is
-// listed and put in order.  A row of 128,256 logits is passed once, and a sixth of it twice for n_top = 20, whatever its order.
+// listed and put in order.  A row is passed once, and n_top 128ths of it twice (20: a sixth, 32: a quarter), whatever its order; where more
+// reach the bound than the list holds, those groups' units are read a third time.
 
 constexpr uint32_t THREADS = 256, WARPS = THREADS / 32, UNROLL = 2, BACK_UNROLL = 1, BACK_PER_SM = 4;
 // Blocks to an SM: four have 64 registers a thread, which a masked pass outgrows (masked rows of 128,256 bf16, us with three and with four, without
@@ -692,7 +693,8 @@ __global__ void __launch_bounds__(THREADS, per_sm(MASK)) logprobs_kernel(const R
 // grad = (p (A + B lp2) + the g of the given tokens) / T with lp2 = log2 p, A = -(sum g + g_H H) and B = -g_H ln 2.  In ordinary rows 1 / T is
 // part of A, B and g; in others, where that may be beyond fp32 (1 / T is up to 2^126, and so may the incoming gradients be), it comes last, and
 // what p = 0 is multiplied with is not looked at.  A row's sizes decide, not a logit's, and the loop costs nothing for it (2,048 rows of 128,256
-// bf16: 166 us, 168 before; 48 rows of 50,001 fp32 with three given tokens 7.3, 7.1 before).
+// bf16: 166 us, 168 before; 48 rows of 50,001 fp32 with three given tokens 7.3, 7.1 before).  A gradient at another address modulo 32 than
+// the logits is written by single values (1,532 us), and each given token is compared with each unit (5: 175 us, 32: 321).
 // The given tokens' own logits decide whether they count: all of a cluster's blocks have read them before the first writes,
 // since the gradient may take the logits' place.
 
